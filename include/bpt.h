@@ -387,6 +387,129 @@ int bpt_stack_bwd(const bpt_graph_t* g, int32_t B, int32_t H, int32_t num_layers
                   size_t fwd_workspace_bytes, const void* d_root, const void* d_tokens, void* dE, float* const* d_rel,
                   const bpt_layer_grads_t* grads, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- The parts of a gated block with rotary positions, beside the layer above --------------------------------
+ * A block in the manner of present language models, around the same attention calls: h = norm(x), projections of
+ * h, rotary positions on Q and K (in place of, or beside, the relative-position table), attention, then in one
+ * pass the norm of the sublayer's output, its gate, the residual sum and the norm before the next sublayer, a
+ * gated feed-forward block, and that pass again.  The calls are asynchronous on `stream`, allocate nothing and
+ * can be captured into a HIP graph; a captured call keeps using the workspace it was given, so graphs that may
+ * run at the same time need one each.  Sizes of zero rows are valid.  All pointers are device pointers that
+ * start on a 16-byte boundary, else BPT_ERR_INVALID_ARG. */
+
+/* Rotary positions: the features of a head are turned in pairs by an angle proportional to the node's position,
+ *   (a, b) -> (a cos t_i - b sin t_i, b cos t_i + a sin t_i),   t_i = pos * w_i,   i = 0 .. rot / 2 - 1,
+ * on the first `rot` features of every head: pair i is features (i, i + rot / 2), or (2 i, 2 i + 1) with
+ * `interleaved`.  The others are copied.  w_i = base^(-2 i / rot), divided by `factor` for contexts longer than
+ * those a model was made for:  with context > 0 only as far as pair i turns slowly,
+ *   w_i' = w_i (keep + (1 - keep) / factor),   keep = (context w_i / (2 pi) - low) / (high - low) within [0, 1],
+ * (a pair that turns at least `high` times over `context` positions is left alone, one that turns at most `low`
+ * times is slowed down by the whole factor), and all pairs with context = 0.  Angles are formed in 64 bits and
+ * reduced to one turn before sine and cosine are taken, so that far positions keep the accuracy of near ones. */
+typedef struct {
+    int32_t B, H, N, D;   /* batch, heads, rows (any count, also 0), head width (D must be 64) */
+    int32_t dtype;        /* bpt_dtype_t of Q, K and the results */
+    int64_t stride_b, stride_h, stride_n;             /* of Q and K, in elements; multiples of 8, not negative */
+    int64_t out_stride_b, out_stride_h, out_stride_n; /* of Qr and Kr; multiples of 8; no two rows may overlap: in the
+                                                         order of their size, each is at least the one before times its
+                                                         count (the smallest at least D) */
+    int32_t rot;          /* turned features of a head: even, 2 .. D */
+    int32_t interleaved;
+    int32_t inverse;      /* nonzero: turn by -t_i, which is the gradient of the call without it */
+    double base;          /* <= 0 selects 10000 */
+    double factor;        /* <= 0 selects 1 */
+    double context;       /* tokens of the original context, 0: slow all pairs alike */
+    double low, high;     /* low < high; both 0 select 1 and 32 */
+} bpt_rotary_t;
+
+/* Qr, Kr = Q, K turned by the positions pos[b * pos_stride_b + n] (fp32: whole numbers up to 2^24 and halves up to
+ * 2^23 are exact; pos_stride_b = 0 shares N positions among the batch; positions must be finite).  K and Kr may both be
+ * NULL.  Qr may be Q itself (and Kr be K) with equal strides; else results must not overlap inputs.  Qr and Kr
+ * must not overlap.  B * N < 2^31, H < 65536. */
+int bpt_rotary(const bpt_rotary_t* s, const float* pos, int64_t pos_stride_b, const void* Q, const void* K, void* Qr,
+               void* Kr, void* stream);
+
+/* pos[row] of every row of the graph, for bpt_rotary: the centre of the tokens that a node stands for, m 2^l + (2^l - 1) / 2
+ * for node (l, m) -- a token's own index, halves for spans -- counted from the start of its own sequence on the
+ * graph of a packed batch (nodes cut short by their sequence's end keep the centre of the whole node, as they have on the
+ * padded tree).  pos: device, num_nodes fp32. */
+int bpt_node_positions(const bpt_graph_t* g, float* pos, void* stream);
+
+typedef enum { BPT_NORM_NONE = 0, BPT_NORM_LAYER = 1, BPT_NORM_RMS = 2 } bpt_norm_t;
+
+/* Norms before and after a sublayer with its gate and the residual sum, for every row:
+ *   y = residual_scale * x + gate * post(branch),     h = pre(y)
+ * `branch` is the sublayer's output, x the residual stream; y is the new stream and h the next sublayer's input.
+ * post and pre are norms over the d features, or nothing:  LAYER: (v - mean) / sqrt(var + eps) * gain + bias (biased
+ * variance), RMS: v / sqrt(mean(v^2) + eps) * gain + bias.  All arithmetic is fp32 from the stored inputs to the
+ * stored results; h is formed from y before y is rounded. */
+typedef struct {
+    int64_t rows;           /* < 2^31 */
+    int32_t d;              /* features, a multiple of 8, 8 .. 4096 */
+    int32_t dtype;          /* bpt_dtype_t of x, branch, gate, y, h and their gradients */
+    int64_t stride;         /* elements between rows of x, branch, y, h and their gradients: >= d, a multiple of 8 */
+    int32_t post, pre;      /* bpt_norm_t */
+    int64_t gate_rows;      /* consecutive rows that share a row of the gate; 0: no gate.  gate is contiguous
+                               [ceil(rows / gate_rows)][d] */
+    float residual_scale;
+    float eps;              /* <= 0 selects 1e-5 */
+} bpt_residual_norm_t;
+
+/* branch may be NULL with post = NONE and gate_rows = 0 (y = residual_scale * x: the norm before the first sublayer).
+ * Gains and biases: fp32 [d], NULL for 1 and 0 (and NULL where the norm is NONE).  y may be NULL where it is not
+ * wanted, h is NULL exactly where pre = NONE.  stats: fp32 [rows][4] (of branch and of y: mean, 1 / deviation) for the
+ * backward, or NULL.  y may be x or branch itself, and h too where it is not y; other overlaps are not allowed. */
+int bpt_residual_norm_fwd(const bpt_residual_norm_t* s, const void* x, const void* branch, const void* gate,
+                          const float* post_gain, const float* post_bias, const float* pre_gain, const float* pre_bias,
+                          void* y, void* h, float* stats, void* stream);
+
+/* Gradients of bpt_residual_norm_fwd, fp32 [d] (d_gate: the tensors' type, the gate's shape); each is NULL exactly
+ * where its parameter is. */
+typedef struct {
+    void* d_gate;
+    float *d_post_gain, *d_post_bias, *d_pre_gain, *d_pre_bias;
+} bpt_residual_norm_grads_t;
+
+/* Backward: given the gradients dy and dh of a scalar with respect to y and h (either may be NULL and counts as zero;
+ * dh is NULL where pre = NONE), writes dx, d_branch (NULL exactly where branch is) and the parameters' gradients.  x,
+ * branch, gate, gains, post_bias and stats as the forward had and left them.  dx and d_branch may be dy or dh themselves;
+ * other overlaps are not allowed.  Column sums are formed in a fixed order: results are run-to-run identical.
+ * workspace: at least bpt_residual_norm_bwd_workspace bytes (SIZE_MAX for a shape that the calls refuse). */
+size_t bpt_residual_norm_bwd_workspace(const bpt_residual_norm_t* s);
+int bpt_residual_norm_bwd(const bpt_residual_norm_t* s, const void* x, const void* branch, const void* gate,
+                          const float* post_gain, const float* post_bias, const float* pre_gain, const float* pre_bias,
+                          const float* stats, const void* dy, const void* dh, void* dx, void* d_branch,
+                          const bpt_residual_norm_grads_t* grads, void* workspace, size_t workspace_bytes, void* stream);
+
+typedef enum { BPT_ACT_SILU = 0, BPT_ACT_GELU = 1, BPT_ACT_RELU = 2 } bpt_activation_t;
+
+/* Gated feed-forward block, bf16:  Y = (act(X Wg) * (X Wu)) Wd  for every row, maps stored as the layer's
+ * ([inputs][outputs], y = x W): Wg, Wu [d][f], Wd [f][d], contiguous.  act: SILU g / (1 + exp(-g)), GELU
+ * g (1 + erf(g / sqrt 2)) / 2, RELU max(0, g).  Products accumulate in fp32; act(X Wg) * (X Wu) is formed from the
+ * fp32 sums and rounded once to bf16, the operand type of the next product, as are its gradients. */
+typedef struct {
+    int64_t rows;           /* < 2^31 */
+    int32_t d, f;           /* multiples of 8, 8 .. 65536 */
+    int32_t dtype;          /* BPT_BF16 (BPT_ERR_UNSUPPORTED otherwise) */
+    int32_t activation;     /* bpt_activation_t */
+    int64_t stride;         /* elements between rows of X, Y and their gradients: >= d, a multiple of 8, < 2^20 */
+    int32_t grad_dtype;     /* bpt_dtype_t of dWg, dWu, dWd: fp32, or rounded to bf16 */
+} bpt_gated_ffn_t;
+
+/* workspace: at least bpt_gated_ffn_fwd_workspace bytes (SIZE_MAX for a shape that the calls refuse); its contents are not
+ * needed by the backward.  Y must not overlap X. */
+size_t bpt_gated_ffn_fwd_workspace(const bpt_gated_ffn_t* s);
+int bpt_gated_ffn_fwd(const bpt_gated_ffn_t* s, const void* X, const void* Wg, const void* Wu, const void* Wd, void* Y,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* Backward: with G = X Wg, U = X Wu formed again (nothing is kept between the calls),  dF = dY Wd^T,
+ * dG = dF * U * act'(G), dU = dF * act(G),  writes  dX = dG Wg^T + dU Wu^T,  dWg = X^T dG, dWu = X^T dU and
+ * dWd = (act(G) * U)^T dY (contiguous, grad_dtype).  act'(0) = 0 for RELU.  Sums over rows are cut into slices that are
+ * added in a fixed order; results are run-to-run identical.  dX may be dY itself, or X; other overlaps are not allowed. */
+size_t bpt_gated_ffn_bwd_workspace(const bpt_gated_ffn_t* s);
+int bpt_gated_ffn_bwd(const bpt_gated_ffn_t* s, const void* X, const void* Wg, const void* Wu, const void* Wd,
+                      const void* dY, void* dX, void* dWg, void* dWu, void* dWd, void* workspace, size_t workspace_bytes,
+                      void* stream);
+
 /* Sec. 3.2 with the rule for shorter sequences stated at the top of this header: the number
  * of edges of the graph over n tokens with density k that a sequence of len tokens keeps
  * (0 <= len <= n; len == n gives the graph's own edge count).  Host arithmetic only, no

@@ -26,7 +26,8 @@ EXPORTS = [
     "bpt_attn_fwd", "bpt_attn_fwd_static", "bpt_attn_bwd", "bpt_attn_bwd_query_side", "bpt_attn_bwd_key_side", "bpt_profile_enable",
     "bpt_profile_report", "bpt_calibrate_gather", "bpt_layer_fwd_workspace", "bpt_layer_fwd", "bpt_layer_bwd_workspace", "bpt_layer_bwd",
     "bpt_stack_fwd_workspace", "bpt_stack_fwd", "bpt_stack_bwd_workspace", "bpt_stack_bwd",
-    "bpt_count_edges", "bpt_strerror",
+    "bpt_count_edges", "bpt_strerror", "bpt_rotary", "bpt_node_positions", "bpt_residual_norm_fwd", "bpt_residual_norm_bwd_workspace",
+    "bpt_residual_norm_bwd", "bpt_gated_ffn_fwd_workspace", "bpt_gated_ffn_fwd", "bpt_gated_ffn_bwd_workspace", "bpt_gated_ffn_bwd",
 ]
 
 
@@ -47,6 +48,28 @@ GRAD_NAMES = ("dWq", "dWk", "dWv", "dWo", "dW1", "db1", "dW2", "db2", "dg1", "db
 
 class BptLayerGrads(ctypes.Structure):
     _fields_ = [(name, ctypes.c_void_p) for name in GRAD_NAMES]
+
+
+class BptRotary(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "H", "N", "D", "dtype")] + \
+               [(n, ctypes.c_int64) for n in ("stride_b", "stride_h", "stride_n", "out_stride_b", "out_stride_h", "out_stride_n")] + \
+               [(n, ctypes.c_int32) for n in ("rot", "interleaved", "inverse")] + \
+               [(n, ctypes.c_double) for n in ("base", "factor", "context", "low", "high")]
+
+
+class BptResidualNorm(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("d", ctypes.c_int32), ("dtype", ctypes.c_int32), ("stride", ctypes.c_int64),
+                ("post", ctypes.c_int32), ("pre", ctypes.c_int32), ("gate_rows", ctypes.c_int64),
+                ("residual_scale", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+class BptResidualNormGrads(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("d_gate", "d_post_gain", "d_post_bias", "d_pre_gain", "d_pre_bias")]
+
+
+class BptGatedFfn(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("d", ctypes.c_int32), ("f", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("activation", ctypes.c_int32), ("stride", ctypes.c_int64), ("grad_dtype", ctypes.c_int32)]
 
 
 class BptError(RuntimeError):
@@ -130,6 +153,24 @@ def load_library() -> ctypes.CDLL:
                                 P(BptLayerGrads), vp, sz, vp]
     L.bpt_count_edges.restype = ctypes.c_int
     L.bpt_count_edges.argtypes = [i32, i32, i32, i32, P(i64)]
+    L.bpt_rotary.restype = ctypes.c_int
+    L.bpt_rotary.argtypes = [P(BptRotary), vp, i64, vp, vp, vp, vp, vp]
+    L.bpt_node_positions.restype = ctypes.c_int
+    L.bpt_node_positions.argtypes = [vp, vp, vp]
+    L.bpt_residual_norm_fwd.restype = ctypes.c_int
+    L.bpt_residual_norm_fwd.argtypes = [P(BptResidualNorm)] + [vp] * 11
+    L.bpt_residual_norm_bwd_workspace.restype = sz
+    L.bpt_residual_norm_bwd_workspace.argtypes = [P(BptResidualNorm)]
+    L.bpt_residual_norm_bwd.restype = ctypes.c_int
+    L.bpt_residual_norm_bwd.argtypes = [P(BptResidualNorm)] + [vp] * 12 + [P(BptResidualNormGrads), vp, sz, vp]
+    L.bpt_gated_ffn_fwd_workspace.restype = sz
+    L.bpt_gated_ffn_fwd_workspace.argtypes = [P(BptGatedFfn)]
+    L.bpt_gated_ffn_fwd.restype = ctypes.c_int
+    L.bpt_gated_ffn_fwd.argtypes = [P(BptGatedFfn)] + [vp] * 6 + [sz, vp]
+    L.bpt_gated_ffn_bwd_workspace.restype = sz
+    L.bpt_gated_ffn_bwd_workspace.argtypes = [P(BptGatedFfn)]
+    L.bpt_gated_ffn_bwd.restype = ctypes.c_int
+    L.bpt_gated_ffn_bwd.argtypes = [P(BptGatedFfn)] + [vp] * 10 + [sz, vp]
     L.bpt_strerror.restype = ctypes.c_char_p
     L.bpt_strerror.argtypes = [ctypes.c_int]
     _lib = L
@@ -659,6 +700,300 @@ def graph_attention(g: Graph, Q, K, V, rel, scale: Optional[float] = None, seq_l
     """out = graph self-attention of eq. (8), differentiable with respect to Q, K, V and rel; dropout = (rate, seed)
     of the dropout on the attention weights (give every call of a training step its own seed)."""
     return GraphAttentionFunction.apply(g, Q, K, V, rel, scale, seq_len, dropout)
+
+
+# ---- the parts of a gated block with rotary positions ---------------------------------------------------------------
+_DTYPES = {torch.float32: BPT_F32, torch.bfloat16: BPT_BF16}
+NORMS = {"none": 0, "layer": 1, "rms": 2}
+ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}
+
+
+def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+def _on_device(x: torch.Tensor, what: str) -> torch.device:
+    """The device of a call's first tensor, which has to be the current one: its stream is the one the call goes to."""
+    dev = x.device
+    if dev.type != "cuda" or dev.index != torch.cuda.current_device():
+        raise ValueError("%s must be on the current cuda device, got %s" % (what, dev))
+    return dev
+
+
+def _rotary_out(x: torch.Tensor) -> torch.Tensor:
+    """A dense [B,H,N,D] tensor with x's order of heads and rows."""
+    B, H, N, D = x.shape
+    if H > 1 and N > 1 and x.stride(1) < x.stride(2):
+        return torch.empty((B, N, H, D), dtype=x.dtype, device=x.device).permute(0, 2, 1, 3)
+    return torch.empty((B, H, N, D), dtype=x.dtype, device=x.device)
+
+
+def bpt_rotary(Q: torch.Tensor, K: Optional[torch.Tensor], pos: torch.Tensor, rot: Optional[int] = None, interleaved: bool = False,
+               base: float = 10000.0, factor: float = 1.0, context: float = 0, low: float = 1.0, high: float = 32.0,
+               inverse: bool = False, out=None):
+    """Qr, Kr = rotary positions on Q and K [B,H,N,64] (K may be None; any strides with the features contiguous): the first
+    `rot` features of every head (all by default) are turned by pos * base^(-2 i / rot), with `factor`, `context`, `low` and
+    `high` for contexts longer than those a model was made for (see include/bpt.h).  pos: fp32 [N] or [B, N].  inverse: the other
+    way, which is the gradient.  out: a pair of tensors to write, which may be (Q, K) themselves."""
+    dev = _on_device(Q, "Q")
+    if Q.dim() != 4 or Q.stride(3) != 1:
+        raise ValueError("Q must be [B,H,N,D] with the features contiguous")
+    dt = _DTYPES.get(Q.dtype)
+    if dt is None:
+        raise ValueError("dtype must be float32 or bfloat16")
+    if K is not None and (K.dtype != Q.dtype or K.shape != Q.shape or K.stride() != Q.stride() or K.device != dev):
+        raise ValueError("Q and K must share dtype, shape, strides and device")
+    B, H, N, D = Q.shape
+    if pos.dtype != torch.float32 or pos.device != dev or tuple(pos.shape) not in ((N,), (B, N)) or (N > 1 and pos.stride(-1) != 1):
+        raise ValueError("pos must be a float32 tensor [N] or [B, N] on the tensors' device with contiguous rows")
+    if out is None:
+        Qr, Kr = _rotary_out(Q), None if K is None else _rotary_out(K)
+    else:
+        Qr, Kr = out
+        if (Kr is None) != (K is None):
+            raise ValueError("out must hold a tensor for each of Q and K")
+        for t in (Qr,) if Kr is None else (Qr, Kr):
+            if t.dtype != Q.dtype or t.shape != Q.shape or t.stride() != Qr.stride() or t.stride(3) != 1 or t.device != dev:
+                raise ValueError("the results must have Q's dtype, shape and device and share strides")
+    s, o = Q.stride(), Qr.stride()
+    shp = BptRotary(B, H, N, D, dt, s[0], s[1], s[2], o[0], o[1], o[2], D if rot is None else int(rot), bool(interleaved), bool(inverse),
+                    base, factor, context, low, high)
+    _check(load_library().bpt_rotary(ctypes.byref(shp), pos.data_ptr(), pos.stride(0) if pos.dim() == 2 else 0, Q.data_ptr(), _ptr(K),
+                                     Qr.data_ptr(), _ptr(Kr), _stream_ptr()), "bpt_rotary")
+    return Qr, Kr
+
+
+def bpt_node_positions(g: Graph) -> torch.Tensor:
+    """fp32 [rows of the graph]: the centre of every node's tokens within its own sequence, for bpt_rotary."""
+    pos = torch.empty(g.num_nodes, dtype=torch.float32, device="cuda")
+    _check(load_library().bpt_node_positions(g.handle, pos.data_ptr(), _stream_ptr()), "bpt_node_positions")
+    return pos
+
+
+def _row_stride(x: torch.Tensor, what: str) -> int:
+    """Elements between the rows of a [..., d] tensor whose rows lie evenly apart."""
+    if x.stride(-1) != 1:
+        raise ValueError("the features of %s must be contiguous" % what)
+    if x.dim() == 1:
+        return x.shape[0]
+    stride = x.stride(-2) if x.shape[-2] > 1 else max(x.stride(-2), x.shape[-1])
+    step = stride * x.shape[-2]
+    for i in range(x.dim() - 3, -1, -1):
+        if x.shape[i] > 1 and x.stride(i) != step:
+            raise ValueError("the rows of %s must lie evenly apart" % what)
+        step *= x.shape[i]
+    return stride
+
+
+def _like(x: torch.Tensor, t: torch.Tensor, what: str) -> None:
+    if t.dtype != x.dtype or t.shape != x.shape or t.stride() != x.stride() or t.device != x.device:
+        raise ValueError("%s must have the dtype, shape, strides and device of x" % what)
+
+
+def _norm_args(x, branch, gate, post, pre, post_gain, post_bias, pre_gain, pre_bias, gate_rows, residual_scale, eps):
+    dev = _on_device(x, "x")
+    dt = _DTYPES.get(x.dtype)
+    if dt is None:
+        raise ValueError("dtype must be float32 or bfloat16")
+    if post not in NORMS or pre not in NORMS:
+        raise ValueError("a norm is one of %s" % sorted(NORMS))
+    d = x.shape[-1]
+    rows = x.numel() // d if d else 0
+    if branch is not None:
+        _like(x, branch, "branch")
+    if (gate is None) != (gate_rows == 0):
+        raise ValueError("gate_rows says how many rows share a row of the gate: 0 without a gate")
+    if gate is not None and (gate.dtype != x.dtype or tuple(gate.shape) != (-(-rows // gate_rows), d) or not gate.is_contiguous() or
+                             gate.device != dev):
+        raise ValueError("gate must be contiguous [%d, %d] with the dtype and device of x" % (-(-rows // gate_rows), d))
+    for name, p in (("post_gain", post_gain), ("post_bias", post_bias), ("pre_gain", pre_gain), ("pre_bias", pre_bias)):
+        if p is not None and (p.dtype != torch.float32 or tuple(p.shape) != (d,) or not p.is_contiguous() or p.device != dev):
+            raise ValueError("%s must be a contiguous float32 tensor [%d] on the device of x" % (name, d))
+    return BptResidualNorm(rows, d, dt, _row_stride(x, "x"), NORMS[post], NORMS[pre], gate_rows, residual_scale, eps)
+
+
+def bpt_residual_norm_fwd(x: torch.Tensor, branch: Optional[torch.Tensor], gate: Optional[torch.Tensor] = None, post: str = "none",
+                          pre: str = "rms", post_gain: Optional[torch.Tensor] = None, post_bias: Optional[torch.Tensor] = None,
+                          pre_gain: Optional[torch.Tensor] = None, pre_bias: Optional[torch.Tensor] = None, gate_rows: int = 0,
+                          residual_scale: float = 1.0, eps: float = 1e-5, want_stats: bool = False):
+    """y = residual_scale * x + gate * post(branch) and h = pre(y), post and pre "layer", "rms" or "none" (then h is None).
+    x, branch: [..., d] in fp32 or bf16, equal layouts; gate: [ceil(rows / gate_rows), d] in their type, each row for gate_rows
+    consecutive rows; gains and biases fp32 [d] or None.  Returns (y, h), with want_stats (y, h, stats) for the backward."""
+    s = _norm_args(x, branch, gate, post, pre, post_gain, post_bias, pre_gain, pre_bias, gate_rows, residual_scale, eps)
+    y = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device)
+    h = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device) if s.pre else None
+    stats = torch.empty((s.rows, 4), dtype=torch.float32, device=x.device) if want_stats else None
+    _check(load_library().bpt_residual_norm_fwd(ctypes.byref(s), x.data_ptr(), _ptr(branch), _ptr(gate), _ptr(post_gain), _ptr(post_bias),
+                                                _ptr(pre_gain), _ptr(pre_bias), y.data_ptr(), _ptr(h), _ptr(stats), _stream_ptr()),
+           "bpt_residual_norm_fwd")
+    return (y, h, stats) if want_stats else (y, h)
+
+
+def bpt_residual_norm_bwd(x: torch.Tensor, branch: Optional[torch.Tensor], gate: Optional[torch.Tensor], stats: torch.Tensor,
+                          dy: Optional[torch.Tensor], dh: Optional[torch.Tensor], post: str = "none", pre: str = "rms",
+                          post_gain: Optional[torch.Tensor] = None, post_bias: Optional[torch.Tensor] = None,
+                          pre_gain: Optional[torch.Tensor] = None, pre_bias: Optional[torch.Tensor] = None, gate_rows: int = 0,
+                          residual_scale: float = 1.0, eps: float = 1e-5) -> dict:
+    """Backward of bpt_residual_norm_fwd, called with the same arguments and the stats it returned; dy or dh may be None.  Returns
+    a dict: dx, and d_branch, d_gate, d_post_gain, d_post_bias, d_pre_gain, d_pre_bias for what was given."""
+    s = _norm_args(x, branch, gate, post, pre, post_gain, post_bias, pre_gain, pre_bias, gate_rows, residual_scale, eps)
+    if dy is None and dh is None:
+        raise ValueError("pass dy, dh or both")
+    for name, t in (("dy", dy), ("dh", dh)):
+        if t is not None:
+            _like(x, t, name)
+    if stats.dtype != torch.float32 or tuple(stats.shape) != (s.rows, 4) or not stats.is_contiguous() or stats.device != x.device:
+        raise ValueError("stats must be what the forward returned")
+    L = load_library()
+    out = {"dx": torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device)}
+    if branch is not None:
+        out["d_branch"] = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device)
+    for name, p in (("d_gate", gate), ("d_post_gain", post_gain), ("d_post_bias", post_bias), ("d_pre_gain", pre_gain),
+                    ("d_pre_bias", pre_bias)):
+        if p is not None:
+            out[name] = torch.empty_like(p)
+    grads = BptResidualNormGrads(*[_ptr(out.get(n)) for n in ("d_gate", "d_post_gain", "d_post_bias", "d_pre_gain", "d_pre_bias")])
+    need = _need(int(L.bpt_residual_norm_bwd_workspace(ctypes.byref(s))), "bpt_residual_norm_bwd_workspace")
+    ws, ws_ptr = _workspace(need, x.device)
+    _check(L.bpt_residual_norm_bwd(ctypes.byref(s), x.data_ptr(), _ptr(branch), _ptr(gate), _ptr(post_gain), _ptr(post_bias),
+                                   _ptr(pre_gain), _ptr(pre_bias), stats.data_ptr(), _ptr(dy), _ptr(dh), out["dx"].data_ptr(),
+                                   _ptr(out.get("d_branch")), ctypes.byref(grads), ws_ptr, need, _stream_ptr()),
+           "bpt_residual_norm_bwd")
+    return out
+
+
+def _ffn_args(X, Wg, Wu, Wd, activation, bf16_grads=False):
+    dev = _on_device(X, "X")
+    if X.dtype != torch.bfloat16:
+        raise ValueError("X must be bfloat16")
+    if activation not in ACTIVATIONS:
+        raise ValueError("an activation is one of %s" % sorted(ACTIVATIONS))
+    d = X.shape[-1]
+    f = Wg.shape[-1]
+    for name, W, shape in (("Wg", Wg, (d, f)), ("Wu", Wu, (d, f)), ("Wd", Wd, (f, d))):
+        if W.dtype != torch.bfloat16 or tuple(W.shape) != shape or not W.is_contiguous() or W.device != dev:
+            raise ValueError("%s must be a contiguous bfloat16 tensor %s on the device of X" % (name, shape))
+    return BptGatedFfn(X.numel() // d if d else 0, d, f, BPT_BF16, ACTIVATIONS[activation], _row_stride(X, "X"),
+                       BPT_BF16 if bf16_grads else BPT_F32)
+
+
+def bpt_gated_ffn_fwd(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.Tensor, activation: str = "silu",
+                      out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Y = (act(X Wg) * (X Wu)) Wd for X [..., d] bf16, Wg, Wu [d, f], Wd [f, d]; act "silu", "gelu" or "relu"."""
+    s = _ffn_args(X, Wg, Wu, Wd, activation)
+    L = load_library()
+    if out is None:
+        out = torch.empty_strided(X.shape, X.stride(), dtype=X.dtype, device=X.device)
+    else:
+        _like(X, out, "out")
+    need = _need(int(L.bpt_gated_ffn_fwd_workspace(ctypes.byref(s))), "bpt_gated_ffn_fwd_workspace")
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=X.device)
+    _check(L.bpt_gated_ffn_fwd(ctypes.byref(s), X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(), out.data_ptr(),
+                               workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_ptr()), "bpt_gated_ffn_fwd")
+    return out
+
+
+def bpt_gated_ffn_bwd(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.Tensor, dY: torch.Tensor, activation: str = "silu",
+                      bf16_grads: bool = False, workspace: Optional[torch.Tensor] = None):
+    """Backward of bpt_gated_ffn_fwd, which forms the hidden activations again: (dX, dWg, dWu, dWd), the weights' gradients in fp32 or,
+    with bf16_grads, rounded to bf16."""
+    s = _ffn_args(X, Wg, Wu, Wd, activation, bf16_grads)
+    _like(X, dY, "dY")
+    L = load_library()
+    dX = torch.empty_strided(X.shape, X.stride(), dtype=X.dtype, device=X.device)
+    dWg, dWu, dWd = (torch.empty(W.shape, dtype=torch.bfloat16 if bf16_grads else torch.float32, device=X.device) for W in (Wg, Wu, Wd))
+    need = _need(int(L.bpt_gated_ffn_bwd_workspace(ctypes.byref(s))), "bpt_gated_ffn_bwd_workspace")
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=X.device)
+    _check(L.bpt_gated_ffn_bwd(ctypes.byref(s), X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(), dY.data_ptr(), dX.data_ptr(),
+                               dWg.data_ptr(), dWu.data_ptr(), dWd.data_ptr(), workspace.data_ptr(),
+                               workspace.numel() * workspace.element_size(), _stream_ptr()), "bpt_gated_ffn_bwd")
+    return dX, dWg, dWu, dWd
+
+
+def _in_layout_of(x: torch.Tensor, g: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
+    """A gradient with the strides and dtype of x, which the calls ask for (autograd hands over any)."""
+    if g is None or (g.stride() == x.stride() and g.dtype == x.dtype):
+        return g
+    return torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device).copy_(g)
+
+
+class RotaryFunction(torch.autograd.Function):
+    """bpt_rotary; its gradient is the same call the other way round."""
+
+    @staticmethod
+    def forward(ctx, Q, K, pos, how):
+        ctx.save_for_backward(pos)
+        ctx.how = how
+        ctx.set_materialize_grads(False)
+        return bpt_rotary(Q, K, pos, **how)
+
+    @staticmethod
+    def backward(ctx, dQ, dK):
+        pos, = ctx.saved_tensors
+        if dQ is not None and dK is not None:
+            return bpt_rotary(dQ.contiguous(), dK.contiguous(), pos, inverse=True, **ctx.how) + (None, None)
+        turned = [None if g is None else bpt_rotary(g.contiguous(), None, pos, inverse=True, **ctx.how)[0] for g in (dQ, dK)]
+        return (*turned, None, None)
+
+
+def rotary(Q: torch.Tensor, K: Optional[torch.Tensor], pos: torch.Tensor, rot: Optional[int] = None, interleaved: bool = False,
+           base: float = 10000.0, factor: float = 1.0, context: float = 0, low: float = 1.0, high: float = 32.0):
+    """bpt_rotary, differentiable with respect to Q and K."""
+    return RotaryFunction.apply(Q, K, pos, dict(rot=rot, interleaved=interleaved, base=base, factor=factor, context=context, low=low,
+                                                high=high))
+
+
+class ResidualNormFunction(torch.autograd.Function):
+    """bpt_residual_norm_fwd / bpt_residual_norm_bwd."""
+
+    @staticmethod
+    def forward(ctx, x, branch, gate, post_gain, post_bias, pre_gain, pre_bias, how):
+        params = dict(post_gain=post_gain, post_bias=post_bias, pre_gain=pre_gain, pre_bias=pre_bias)
+        y, h, stats = bpt_residual_norm_fwd(x, branch, gate, want_stats=True, **params, **how)
+        ctx.save_for_backward(x, branch, gate, stats, *params.values())
+        ctx.how = how
+        ctx.set_materialize_grads(False)
+        return y, h
+
+    @staticmethod
+    def backward(ctx, dy, dh):
+        x, branch, gate, stats, post_gain, post_bias, pre_gain, pre_bias = ctx.saved_tensors
+        if dy is None and dh is None:
+            return (None,) * 8
+        g = bpt_residual_norm_bwd(x, branch, gate, stats, _in_layout_of(x, dy), _in_layout_of(x, dh), post_gain=post_gain,
+                                  post_bias=post_bias, pre_gain=pre_gain, pre_bias=pre_bias, **ctx.how)
+        return (g["dx"],) + tuple(g.get("d_" + n) for n in ("branch", "gate", "post_gain", "post_bias", "pre_gain", "pre_bias")) + (None,)
+
+
+def residual_norm(x: torch.Tensor, branch: Optional[torch.Tensor], gate: Optional[torch.Tensor] = None, post: str = "none", pre: str = "rms",
+                  post_gain: Optional[torch.Tensor] = None, post_bias: Optional[torch.Tensor] = None,
+                  pre_gain: Optional[torch.Tensor] = None, pre_bias: Optional[torch.Tensor] = None, gate_rows: int = 0,
+                  residual_scale: float = 1.0, eps: float = 1e-5):
+    """(y, h) of bpt_residual_norm_fwd, differentiable with respect to all tensors."""
+    return ResidualNormFunction.apply(x, branch, gate, post_gain, post_bias, pre_gain, pre_bias,
+                                      dict(post=post, pre=pre, gate_rows=gate_rows, residual_scale=residual_scale, eps=eps))
+
+
+class GatedFfnFunction(torch.autograd.Function):
+    """bpt_gated_ffn_fwd / bpt_gated_ffn_bwd: only the inputs are kept between the two; gradients leave in bf16, the inputs' type."""
+
+    @staticmethod
+    def forward(ctx, X, Wg, Wu, Wd, activation):
+        ctx.save_for_backward(X, Wg, Wu, Wd)
+        ctx.activation = activation
+        return bpt_gated_ffn_fwd(X, Wg, Wu, Wd, activation)
+
+    @staticmethod
+    def backward(ctx, dY):
+        X, Wg, Wu, Wd = ctx.saved_tensors
+        return bpt_gated_ffn_bwd(X, Wg, Wu, Wd, _in_layout_of(X, dY), ctx.activation, bf16_grads=True) + (None,)
+
+
+def gated_ffn(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.Tensor, activation: str = "silu") -> torch.Tensor:
+    """bpt_gated_ffn_fwd, differentiable with respect to X and the weights."""
+    return GatedFfnFunction.apply(X, Wg, Wu, Wd, activation)
 
 
 def bpt_profile_enable(on: bool) -> None:

@@ -1,0 +1,189 @@
+// Tiles of a matrix product C[m][n] = sum_k A[m][k] B[k][n] on the matrix cores, for the feed-forward block: bf16 operands,
+// fp32 sums.  A workgroup computes BM x BN of C in WR x WC wavefronts; both operands go through LDS in slabs of 64 k,
+// two slabs deep, loaded straight into LDS (no registers in between).
+//
+// An operand lies in memory with either k or its own index (m or n) contiguous, and is kept that way in LDS:
+//   k contiguous     [W][64]  128 bytes per row, read 16 bytes per lane (8 k of one row)
+//   index contiguous [64][W]  read with the transposing LDS reads, which hand a lane 4 k of one column
+// Either image is permuted within a row (16-byte pieces by the row's low bits, 32-byte pieces by the k's) so that the
+// lanes of one read fall into different banks; direct loads write LDS in lane order, so the permutation is applied to
+// the addresses they read from.
+//
+// Pieces outside the matrices (rows past m or n, k past K) are requested at an offset that the buffer descriptor's
+// bound refuses, which reads as zero.
+#pragma once
+
+#include "row_device.h"
+
+namespace bpt {
+namespace {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef short i16x4_t __attribute__((ext_vector_type(4)));
+typedef short i16x8_t __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) unsigned char* lds_bytes_t;
+
+constexpr int kSlab = 64;                       // k per slab
+constexpr int kBound = 0x7FFFFFF0;              // bytes an operand's descriptor covers from its tile's first element
+constexpr int kOutside = (int)0x80000000;       // an offset behind it
+
+// permutation of the 32-byte pieces of a row of W elements (index contiguous): the 4 k of a transposing read fall into
+// different pairs of pieces
+template <int W>
+__device__ __forceinline__ int piece_swap(int k) {
+    return W >= 128 ? 2 * (k & 3) : W == 64 ? (k & 3) : (k & 1);
+}
+
+// Loads a slab of an operand of W rows (or columns) into LDS with WAVES wavefronts.
+template <int W, int WAVES, bool KFIRST>   // KFIRST: k contiguous
+struct SlabLoader {
+    static constexpr int kBytes = W * kSlab * 2;
+    static constexpr int kLoads = kBytes / 1024 / WAVES;   // 1 KB per wavefront and instruction
+    static_assert(kLoads * 1024 * WAVES == kBytes, "the wavefronts share the slab evenly");
+    int off[kLoads];
+
+    // position of a lane's piece: its index within the W and its first k
+    static __device__ __forceinline__ void place(int i, int wave, int lane, int& index, int& k) {
+        const int q = (i * WAVES + wave) * 64 + lane;
+        if (KFIRST) {
+            index = q >> 3;
+            k = ((q & 7) ^ (index & 7)) * 8;
+        } else {
+            constexpr int kPieces = W / 8;
+            k = q / kPieces;
+            const int p = q % kPieces;
+            index = ((((p >> 1) ^ piece_swap<W>(k)) << 1) | (p & 1)) * 8;
+        }
+    }
+    // ld: elements between rows as stored; valid: how many of the W indexes exist
+    __device__ __forceinline__ void init(int wave, int lane, int64_t ld, int64_t valid) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            int index, k;
+            place(i, wave, lane, index, k);
+            const int at = KFIRST ? index * (int)ld + k : k * (int)ld + index;
+            off[i] = index < valid ? at * 2 : kOutside;
+        }
+    }
+    // p: the tile's first element of this slab; k_left: k that exist from there on
+    __device__ __forceinline__ void load(const bf16_t* p, int64_t k_left, lds_bytes_t lds, int wave, int lane) const {
+        __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(p), 0, kBound, 0x00020000);
+        if (k_left >= kSlab) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + (i * WAVES + wave) * 1024), 16, off[i], 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                int index, k;
+                place(i, wave, lane, index, k);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + (i * WAVES + wave) * 1024), 16,
+                                                         k < k_left ? off[i] : kOutside, 0, 0, 0);
+            }
+        }
+    }
+};
+
+// Operand of v_mfma_f32_32x32x16_bf16: lane l holds k = 16 kk + 8 (l / 32) .. + 7 of index first + l % 32.
+template <int W, bool KFIRST>
+__device__ __forceinline__ bf16x8_t fragment(lds_bytes_t slab, int first, int kk, int lane) {
+    if constexpr (KFIRST) {
+        typedef __attribute__((address_space(3))) const bf16x8_t* ptr_t;
+        return *(ptr_t)(slab + (first + (lane & 31)) * 128 + (((kk * 2 + (lane >> 5)) ^ (lane & 7)) * 16));
+    } else {
+        typedef __attribute__((address_space(3))) i16x4_t* ptr_t;
+        const int k = kk * 16 + (lane >> 5) * 8 + ((lane & 15) >> 2);
+        const int piece = ((first >> 4) + ((lane >> 4) & 1)) ^ piece_swap<W>((lane & 15) >> 2);
+        lds_bytes_t p = slab + k * (W * 2) + piece * 32 + (lane & 3) * 8;
+        const i16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ptr_t)p);
+        const i16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ptr_t)(p + 4 * W * 2));
+        const i16x8_t xy = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+        return __builtin_bit_cast(bf16x8_t, xy);
+    }
+}
+
+// One operand pair of a tile.  PAIR: B is two matrices of BN / 2 columns each, whose slabs lie one behind the other; a
+// wavefront then computes the same columns of both (the first half of its column blocks are of the first).
+template <int BM, int BN, int WR, int WC, bool A_KFIRST, bool B_KFIRST, bool PAIR>
+struct Tile {
+    static constexpr int kWaves = WR * WC, kThreads = 64 * kWaves;
+    static constexpr int kRows = BM / WR / 32;                 // 32-row blocks of a wavefront
+    static constexpr int kCols = BN / WC / 32;                 // 32-column blocks
+    static constexpr int kBWidth = PAIR ? BN / 2 : BN;
+    using LoadA = SlabLoader<BM, kWaves, A_KFIRST>;
+    using LoadB = SlabLoader<kBWidth, kWaves, B_KFIRST>;
+    static constexpr int kStage = LoadA::kBytes + LoadB::kBytes * (PAIR ? 2 : 1);
+    static constexpr int kLds = 2 * kStage;
+    typedef f32x16_t Acc[kRows][kCols];
+
+    LoadA la;
+    LoadB lb;
+    lds_bytes_t lds;
+    int wave, lane, wr, wc;
+
+    __device__ __forceinline__ void init(unsigned char* shared, int64_t lda, int64_t rows_valid, int64_t ldb, int64_t cols_valid) {
+        lds = (lds_bytes_t)shared;
+        lane = threadIdx.x & 63;
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        wr = wave / WC;
+        wc = wave % WC;
+        la.init(wave, lane, lda, rows_valid);
+        lb.init(wave, lane, ldb, cols_valid);
+    }
+    // first column, within the tile's BN (PAIR: within either half), of a column block of this wavefront
+    __device__ __forceinline__ int col_of(int j) const {
+        return PAIR ? (wc * (kCols / 2) + j % (kCols / 2)) * 32 : (wc * kCols + j) * 32;
+    }
+    __device__ __forceinline__ int row_of(int i) const { return (wr * kRows + i) * 32; }
+
+    __device__ __forceinline__ void load(const bf16_t* a, const bf16_t* b0, const bf16_t* b1, int64_t k_left, int stage) const {
+        lds_bytes_t p = lds + stage * kStage;
+        la.load(a, k_left, p, wave, lane);
+        lb.load(b0, k_left, p + LoadA::kBytes, wave, lane);
+        if (PAIR) lb.load(b1, k_left, p + LoadA::kBytes + LoadB::kBytes, wave, lane);
+    }
+    __device__ __forceinline__ void multiply(Acc& acc, int stage) const {
+        lds_bytes_t pa = lds + stage * kStage, pb = pa + LoadA::kBytes;
+#pragma unroll
+        for (int kk = 0; kk < kSlab / 16; ++kk) {
+            bf16x8_t a[kRows], b[kCols];
+#pragma unroll
+            for (int j = 0; j < kCols; ++j) {
+                lds_bytes_t p = PAIR && j >= kCols / 2 ? pb + LoadB::kBytes : pb;
+                b[j] = fragment<kBWidth, B_KFIRST>(p, col_of(j), kk, lane);
+            }
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) a[i] = fragment<BM, A_KFIRST>(pa, row_of(i), kk, lane);
+#pragma unroll
+            for (int i = 0; i < kRows; ++i)
+#pragma unroll
+                for (int j = 0; j < kCols; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[j], a[i], acc[i][j], 0, 0, 0);
+        }
+    }
+    // Sum over `slabs` slabs; from(t, a, b0, b1, k_left) says where slab t lies.  All threads call it; on return the
+    // slabs' memory is free.
+    template <typename From>
+    __device__ __forceinline__ void run(Acc& acc, int slabs, From from) const {
+        const bf16_t *a, *b0, *b1 = nullptr;
+        int64_t k_left;
+        if (slabs > 0) {
+            from(0, a, b0, b1, k_left);
+            load(a, b0, b1, k_left, 0);
+        }
+        __syncthreads();
+        for (int t = 0; t < slabs; ++t) {
+            if (t + 1 < slabs) {
+                from(t + 1, a, b0, b1, k_left);
+                load(a, b0, b1, k_left, (t + 1) & 1);
+            }
+            multiply(acc, t & 1);
+            __syncthreads();
+        }
+    }
+};
+// acc[i][j] register r of lane l is C[row_of(i) + l % 32][col_of(j) + 8 (r / 4) + 4 (l / 32) + r % 4]: the matrix
+// instruction is given B as its first operand, so that a lane holds four neighbours of a row of C.
+
+}  // namespace
+}  // namespace bpt
