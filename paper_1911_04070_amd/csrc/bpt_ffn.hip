@@ -244,7 +244,7 @@ ProductPlan plan_product(int64_t M, int64_t N, int64_t K, int terms, int matrice
         p.big = b == 256;
         p.tiles_m = (int)((M + b - 1) / b);
         p.tiles_n = (int)((N + b - 1) / b);
-        const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * matrices, slabs = (K + kSlab - 1) / kSlab * terms;
+        const int64_t tiles = std::max<int64_t>(1, (int64_t)p.tiles_m * p.tiles_n * matrices), slabs = (K + kSlab - 1) / kSlab * terms;
         int64_t s = std::min<int64_t>(kMaxSlices, std::max<int64_t>(1, std::min(want / tiles, slabs * kSlab / kMinSlice)));
         p.slice_slabs = (int)std::max<int64_t>(1, (slabs + s - 1) / s);
         p.slices = (int)std::max<int64_t>(1, (slabs + p.slice_slabs - 1) / p.slice_slabs);

@@ -187,7 +187,7 @@ int bpt_rotary(const bpt_rotary_t* s, const float* pos, int64_t pos_stride_b, co
     const double base = s->base > 0 ? s->base : 10000.0, factor = s->factor > 0 ? s->factor : 1.0;
     const double low = s->low == 0 && s->high == 0 ? 1.0 : s->low, high = s->low == 0 && s->high == 0 ? 32.0 : s->high;
     if (!(std::isfinite(base) && std::isfinite(factor) && std::isfinite(s->context) && s->context >= 0 && low < high) ||
-        !std::isfinite(high - low) || pos_stride_b < 0)
+        !std::isfinite(high - low) || std::isnan(s->base) || std::isnan(s->factor) || pos_stride_b < 0)
         return BPT_ERR_INVALID_ARG;
     const int64_t rows = (int64_t)s->B * s->N;
     if (rows >= INT32_MAX || s->H > 65535) return BPT_ERR_UNSUPPORTED;
