@@ -11,10 +11,11 @@ namespace bpt {
 namespace {
 
 // act(g) and act'(g)
+// (v_exp_f32 and v_rcp_f32 are good to 1 unit in the last place; the results are rounded to bf16)
 template <int ACT>
 __device__ __forceinline__ void activation(float g, float& value, float& slope) {
     if constexpr (ACT == BPT_ACT_SILU) {
-        const float s = 1.f / (1.f + __expf(-g));
+        const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(g * -1.44269504088896341f));
         value = g * s;
         slope = s * (1.f + g * (1.f - s));
     } else if constexpr (ACT == BPT_ACT_GELU) {
@@ -40,9 +41,6 @@ __device__ __forceinline__ void tile_of(int id, int tiles_m, int tiles_n, int& t
     tn = in / rows;
 }
 
-__device__ __forceinline__ void store4(bf16_t* p, float a, float b, float c, float d) {
-    *reinterpret_cast<uint2*>(p) = make_uint2(bf16_pair(a, b), bf16_pair(c, d));
-}
 __device__ __forceinline__ void store4(float* p, float a, float b, float c, float d) {
     *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
 }
@@ -54,32 +52,32 @@ struct UpArgs {
     int64_t M, ldx;
     int32_t d, f, tiles_m, tiles_n;
 };
-template <typename C, int BM, int BN, int ACT>
+template <typename C, int ACT>
 __global__ void __launch_bounds__(C::kThreads, 2) gated_up_kernel(const UpArgs g) {
     __shared__ __attribute__((aligned(1024))) unsigned char shared[C::kLds];
     int tm, tn;
     tile_of(blockIdx.x, g.tiles_m, g.tiles_n, tm, tn);
-    const int64_t m0 = (int64_t)tm * BM;
-    const int n0 = tn * (BN / 2);
+    const int64_t m0 = (int64_t)tm * C::kBM;
+    const int n0 = tn * (C::kBN / 2);
     C t;
     t.init(shared, g.ldx, g.M - m0, g.f, g.f - n0);
     typename C::Acc acc = {};
     const bf16_t *X = g.X + m0 * g.ldx, *Wg = g.Wg + n0, *Wu = g.Wu + n0;
-    t.run(acc, (g.d + kSlab - 1) / kSlab, [&](int s, const bf16_t*& a, const bf16_t*& b0, const bf16_t*& b1, int64_t& k_left) {
-        a = X + s * kSlab;
-        b0 = Wg + (int64_t)s * kSlab * g.f;
-        b1 = Wu + (int64_t)s * kSlab * g.f;
-        k_left = g.d - s * kSlab;
+    t.run(acc, (g.d + C::kSlab - 1) / C::kSlab, [&](int s, const bf16_t*& a, const bf16_t*& b0, const bf16_t*& b1, int64_t& k_left) {
+        a = X + s * C::kSlab;
+        b0 = Wg + (int64_t)s * C::kSlab * g.f;
+        b1 = Wu + (int64_t)s * C::kSlab * g.f;
+        k_left = g.d - s * C::kSlab;
     });
     constexpr int kHalf = C::kCols / 2;
+    const RowBlock<kHalf * 32> block(t.lds, t.wave, t.lane);
+    const int col = n0 + t.col_of(0);
 #pragma unroll
     for (int i = 0; i < C::kRows; ++i) {
-        const int64_t m = m0 + t.row_of(i) + (t.lane & 31);
 #pragma unroll
         for (int j = 0; j < kHalf; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int n = n0 + t.col_of(j) + 8 * q + 4 * (t.lane >> 5);
                 float v[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -87,79 +85,135 @@ __global__ void __launch_bounds__(C::kThreads, 2) gated_up_kernel(const UpArgs g
                     activation<ACT>(acc[i][j][4 * q + e], value, slope);
                     v[e] = value * acc[i][kHalf + j][4 * q + e];
                 }
-                if (m < g.M && n < g.f) store4(g.F + m * g.f + n, v[0], v[1], v[2], v[3]);
+                block.put(j * 32 + 8 * q, v[0], v[1], v[2], v[3]);
             }
+        const int64_t m = m0 + t.row_of(i);
+        block.write(g.F + m * g.f + col, g.f, g.M - m, g.f - col);
     }
 }
 
-// ---- C = A0 B0 (+ A1 B1), or several products side by side, in slices of k -----------------------------------
+// ---- C = A0 B0 (+ A1 B1), or several products side by side ------------------------------------------------------
+// The first `full` tiles are computed whole; what is left over is less than the device holds at once and is cut into
+// `slices` of k, whose sums go to `part` and are added by product_sum_kernel, in order.
 struct ProductArgs {
     const bf16_t *A[2], *B[2];
     void* C[2];
     int64_t M, lda, ldb, ldc;
     int64_t K;               // of each of the `terms` products that are added up
     int32_t N, terms, matrices;   // matrices: products with the same A (terms = 1), one behind the other in the grid
-    int32_t tiles_m, tiles_n, slices, slice_slabs;
-    float* part;             // [slices][matrices][M][N], with slices > 1
+    int32_t tiles_m, tiles_n;     // (tiles_n: of one matrix)
+    int32_t full, slices, slice_slabs;
+    float4* part;            // [left-over tile][slice][block of 32 x 32][4][thread]: as the threads hold the sums
 };
-template <typename C, int BM, int BN, bool A_KFIRST, bool B_KFIRST, typename T>
+struct ProductTile {
+    int mat, n0;
+    int64_t m0;
+};
+template <typename C>
+__device__ __forceinline__ ProductTile product_tile(const ProductArgs& g, int id) {
+    int tm, tn;
+    tile_of(id, g.tiles_m, g.tiles_n * g.matrices, tm, tn);
+    const int mat = tn / g.tiles_n;
+    return {mat, (tn - mat * g.tiles_n) * C::kBN, (int64_t)tm * C::kBM};
+}
+template <typename C, bool A_KFIRST, bool B_KFIRST, typename T>
 __global__ void __launch_bounds__(C::kThreads, 2) product_kernel(const ProductArgs g) {
     __shared__ __attribute__((aligned(1024))) unsigned char shared[C::kLds];
-    int tm, tn;
-    tile_of(blockIdx.x, g.tiles_m, g.tiles_n * g.matrices, tm, tn);
-    const int mat = tn / g.tiles_n;
-    tn -= mat * g.tiles_n;
-    const int64_t m0 = (int64_t)tm * BM;
-    const int n0 = tn * BN;
+    const int over = max((int)blockIdx.x - g.full, 0), slice = (int)blockIdx.x < g.full ? 0 : over % g.slices;
+    const bool whole = (int)blockIdx.x < g.full || g.slices == 1;
+    const ProductTile at = product_tile<C>(g, min((int)blockIdx.x, g.full) + over / g.slices);
     C t;
-    t.init(shared, g.lda, g.M - m0, g.ldb, g.N - n0);
+    t.init(shared, g.lda, g.M - at.m0, g.ldb, g.N - at.n0);
     typename C::Acc acc = {};
-    const int64_t a_at = A_KFIRST ? m0 * g.lda : m0, b_at = B_KFIRST ? n0 * g.ldb : n0;
-    const int each = (int)((g.K + kSlab - 1) / kSlab);
-    const int first = blockIdx.y * g.slice_slabs, last = min(first + g.slice_slabs, each * g.terms);
+    const int64_t a_at = A_KFIRST ? at.m0 * g.lda : at.m0, b_at = B_KFIRST ? at.n0 * g.ldb : at.n0;
+    const int each = (int)((g.K + C::kSlab - 1) / C::kSlab), slabs = each * g.terms;
+    const int first = whole ? 0 : slice * g.slice_slabs, last = whole ? slabs : min(first + g.slice_slabs, slabs);
     t.run(acc, max(last - first, 0), [&](int s, const bf16_t*& a, const bf16_t*& b0, const bf16_t*& b1, int64_t& k_left) {
         s += first;
         const int term = s >= each ? 1 : 0;
-        const int64_t k = (int64_t)(s - term * each) * kSlab;
+        const int64_t k = (int64_t)(s - term * each) * C::kSlab;
         a = g.A[term] + a_at + (A_KFIRST ? k : k * g.lda);
-        b0 = g.B[term + mat] + b_at + (B_KFIRST ? k : k * g.ldb);
+        b0 = g.B[term + at.mat] + b_at + (B_KFIRST ? k : k * g.ldb);
         k_left = g.K - k;
     });
-    float* part = g.part + ((int64_t)blockIdx.y * g.matrices + mat) * g.M * g.N;
-    T* out = static_cast<T*>(g.C[mat]);
+    if (!whole) {
+        float4* part = g.part + (int64_t)over * C::kBlocks * 4 * C::kThreads + threadIdx.x;
 #pragma unroll
-    for (int i = 0; i < C::kRows; ++i) {
-        const int64_t m = m0 + t.row_of(i) + (t.lane & 31);
+        for (int i = 0; i < C::kRows; ++i)
 #pragma unroll
-        for (int j = 0; j < C::kCols; ++j)
+            for (int j = 0; j < C::kCols; ++j)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int n = n0 + t.col_of(j) + 8 * q + 4 * (t.lane >> 5);
-                const f32x16_t& x = acc[i][j];
-                if (m < g.M && n < g.N) {
-                    if (g.slices > 1) store4(part + m * g.N + n, x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
-                    else store4(out + m * g.ldc + n, x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
+                for (int q = 0; q < 4; ++q)
+                    part[((i * C::kCols + j) * 4 + q) * C::kThreads] =
+                        make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+        return;
+    }
+    const int col = at.n0 + t.col_of(0);
+    if constexpr (sizeof(T) == 2) {
+        const RowBlock<C::kCols * 32> block(t.lds, t.wave, t.lane);
+#pragma unroll
+        for (int i = 0; i < C::kRows; ++i) {
+#pragma unroll
+            for (int j = 0; j < C::kCols; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    block.put(j * 32 + 8 * q, acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+            const int64_t m = at.m0 + t.row_of(i);
+            block.write(static_cast<bf16_t*>(g.C[at.mat]) + m * g.ldc + col, g.ldc, g.M - m, g.N - col);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < C::kRows; ++i) {
+            const int64_t m = at.m0 + t.row_of(i) + (t.lane & 31);
+            float* out = static_cast<float*>(g.C[at.mat]) + m * g.ldc;
+#pragma unroll
+            for (int j = 0; j < C::kCols; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int n = col + j * 32 + 8 * q + 4 * (t.lane >> 5);
+                    if (m < g.M && n < g.N) store4(out + n, acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
                 }
-            }
+        }
     }
 }
 
-// C = sum of the slices, in order, 4 values per thread
-template <typename T>
-__global__ void __launch_bounds__(256) product_sum_kernel(const float* __restrict__ part, int slices, int64_t elems, int N, int64_t ldc,
-                                                          T* C0, T* C1) {
-    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-    if (i >= elems) return;
-    const int matrices = gridDim.y;
-    const float* p = part + blockIdx.y * elems + i;
-    float4 acc = *reinterpret_cast<const float4*>(p);
+// The left-over tiles: sums of their slices in order; a workgroup takes one 32 x 32 block of each wavefront.
+template <typename C, typename T>
+__global__ void __launch_bounds__(C::kThreads) product_sum_kernel(const ProductArgs g) {
+    __shared__ __attribute__((aligned(1024))) unsigned char shared[RowBlock<32>::kBytes * C::kWaves];
+    const ProductTile at = product_tile<C>(g, g.full + blockIdx.x);
+    C t;
+    t.place(shared);
+    const int i = blockIdx.y / C::kCols, j = blockIdx.y % C::kCols;
+    const int64_t pitch = (int64_t)C::kBlocks * 4 * C::kThreads;
+    const float4* p = g.part + blockIdx.x * g.slices * pitch + blockIdx.y * 4 * C::kThreads + threadIdx.x;
+    float4 x[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) x[q] = p[q * C::kThreads];
 #pragma unroll 4
-    for (int s = 1; s < slices; ++s) {
-        const float4 v = *reinterpret_cast<const float4*>(p + (int64_t)s * matrices * elems);
-        acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
+    for (int s = 1; s < g.slices; ++s) {
+        p += pitch;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float4 v = p[q * C::kThreads];
+            x[q].x += v.x; x[q].y += v.y; x[q].z += v.z; x[q].w += v.w;
+        }
     }
-    const int64_t row = i / N;
-    store4((blockIdx.y ? C1 : C0) + row * ldc + (i - row * N), acc.x, acc.y, acc.z, acc.w);
+    const int col = at.n0 + t.col_of(j);
+    if constexpr (sizeof(T) == 2) {
+        const int64_t m = at.m0 + t.row_of(i);
+        const RowBlock<32> block(t.lds, t.wave, t.lane);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) block.put(8 * q, x[q].x, x[q].y, x[q].z, x[q].w);
+        block.write(static_cast<bf16_t*>(g.C[at.mat]) + m * g.ldc + col, g.ldc, g.M - m, g.N - col);
+    } else {
+        const int64_t m = at.m0 + t.row_of(i) + (t.lane & 31);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int n = col + 8 * q + 4 * (t.lane >> 5);
+            if (m < g.M && n < g.N) store4(static_cast<float*>(g.C[at.mat]) + m * g.ldc + n, x[q].x, x[q].y, x[q].z, x[q].w);
+        }
+    }
 }
 
 // ---- backward up to the hidden gradients ----------------------------------------------------------------------
@@ -170,25 +224,25 @@ struct HiddenArgs {
     int32_t d, f, tiles_m, tiles_n;
 };
 // G = X Wg and U = X Wu are formed again, then dF = dY Wd^T on the same tile: F, dG and dU are written, rounded once.
-template <typename C, typename C2, int BM, int BN, int ACT>
+template <typename C, typename C2, int ACT>
 __global__ void __launch_bounds__(C::kThreads, 2) gated_hidden_bwd_kernel(const HiddenArgs g) {
     __shared__ __attribute__((aligned(1024))) unsigned char shared[C::kLds > C2::kLds ? C::kLds : C2::kLds];
     int tm, tn;
     tile_of(blockIdx.x, g.tiles_m, g.tiles_n, tm, tn);
-    const int64_t m0 = (int64_t)tm * BM;
-    const int n0 = tn * (BN / 2);
+    const int64_t m0 = (int64_t)tm * C::kBM;
+    const int n0 = tn * (C::kBN / 2);
     constexpr int kHalf = C::kCols / 2;
     typename C::Acc gu = {};
-    const int slabs = (g.d + kSlab - 1) / kSlab;
+    const int slabs = (g.d + C::kSlab - 1) / C::kSlab;
     {
         C t;
         t.init(shared, g.ldx, g.M - m0, g.f, g.f - n0);
         const bf16_t *X = g.X + m0 * g.ldx, *Wg = g.Wg + n0, *Wu = g.Wu + n0;
         t.run(gu, slabs, [&](int s, const bf16_t*& a, const bf16_t*& b0, const bf16_t*& b1, int64_t& k_left) {
-            a = X + s * kSlab;
-            b0 = Wg + (int64_t)s * kSlab * g.f;
-            b1 = Wu + (int64_t)s * kSlab * g.f;
-            k_left = g.d - s * kSlab;
+            a = X + s * C::kSlab;
+            b0 = Wg + (int64_t)s * C::kSlab * g.f;
+            b1 = Wu + (int64_t)s * C::kSlab * g.f;
+            k_left = g.d - s * C::kSlab;
         });
     }
     C2 t;
@@ -196,117 +250,158 @@ __global__ void __launch_bounds__(C::kThreads, 2) gated_hidden_bwd_kernel(const 
     typename C2::Acc df = {};
     const bf16_t *dY = g.dY + m0 * g.ldx, *Wd = g.Wd + (int64_t)n0 * g.d;
     t.run(df, slabs, [&](int s, const bf16_t*& a, const bf16_t*& b0, const bf16_t*& b1, int64_t& k_left) {
-        a = dY + s * kSlab;
-        b0 = Wd + s * kSlab;
-        k_left = g.d - s * kSlab;
+        a = dY + s * C::kSlab;
+        b0 = Wd + s * C::kSlab;
+        k_left = g.d - s * C::kSlab;
     });
+    // the three results, one behind the other through the same LDS; G and U make way for act(G) and U act'(G)
+    const RowBlock<kHalf * 32> block(t.lds, t.wave, t.lane);
+    const int col = n0 + t.col_of(0);
 #pragma unroll
     for (int i = 0; i < C::kRows; ++i) {
-        const int64_t m = m0 + t.row_of(i) + (t.lane & 31);
+        const int64_t m = m0 + t.row_of(i), at = m * g.f + col;
 #pragma unroll
         for (int j = 0; j < kHalf; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int n = n0 + t.col_of(j) + 8 * q + 4 * (t.lane >> 5);
-                float vf[4], vg[4], vu[4];
+                float v[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     float value, slope;
-                    const float u = gu[i][kHalf + j][4 * q + e], x = df[i][j][4 * q + e];
+                    const float up = gu[i][kHalf + j][4 * q + e];
                     activation<ACT>(gu[i][j][4 * q + e], value, slope);
-                    vf[e] = value * u;
-                    vg[e] = x * u * slope;
-                    vu[e] = x * value;
+                    v[e] = value * up;
+                    gu[i][j][4 * q + e] = value;
+                    gu[i][kHalf + j][4 * q + e] = up * slope;
                 }
-                if (m < g.M && n < g.f) {
-                    const int64_t at = m * g.f + n;
-                    store4(g.F + at, vf[0], vf[1], vf[2], vf[3]);
-                    store4(g.dG + at, vg[0], vg[1], vg[2], vg[3]);
-                    store4(g.dU + at, vu[0], vu[1], vu[2], vu[3]);
-                }
+                block.put(j * 32 + 8 * q, v[0], v[1], v[2], v[3]);
             }
+        block.write(g.F + at, g.f, g.M - m, g.f - col);
+#pragma unroll
+        for (int half = 1; half >= 0; --half) {
+#pragma unroll
+            for (int j = 0; j < kHalf; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float v[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = df[i][j][4 * q + e] * gu[i][half * kHalf + j][4 * q + e];
+                    block.put(j * 32 + 8 * q, v[0], v[1], v[2], v[3]);
+                }
+            block.write((half ? g.dG : g.dU) + at, g.f, g.M - m, g.f - col);
+        }
     }
 }
 
 // ---- host side --------------------------------------------------------------------------------------------------
 constexpr int kCus = 256;
 
-// tiles of 256 x 256 where they, with slices of at least kMinSlice k, fill three quarters of the compute units, else
-// 128 x 128 (two workgroups per compute unit)
-constexpr int kMinSlice = 512, kMaxSlices = 32;
-struct ProductPlan {
-    bool big;
-    int tiles_m, tiles_n, slices, slice_slabs;
+// Sizes of a workgroup's tile.  kBig: 256 x 256, slabs of 64, one workgroup of 8 wavefronts per compute unit; kWide: 128 x 256,
+// slabs of 32, three deep, and kMid: 128 x 128, slabs of 64: two workgroups of 4 wavefronts per compute unit, of which
+// one multiplies while the other starts up or writes.
+enum TileSize { kBig, kWide, kMid };
+struct TileCost {
+    int m, n, slab, per_cu;
+    float us;        // of 64 k, all compute units busy
 };
+constexpr TileCost kTileCost[] = {{256, 256, 64, 1, 2.1f}, {128, 256, 32, 2, 2.35f}, {128, 128, 64, 2, 1.25f}};
+constexpr float kStartUs = 3.f;              // a tile's first loads and its results
+constexpr float kSumUs = 5.f, kSumBytesPerUs = 4.0e6f;   // adding up slices: a launch, and their bytes written and read
+constexpr int kMaxSlices = 32, kMinSliceK = 128;
+
+struct ProductPlan {
+    TileSize size;
+    int tiles_m, tiles_n, full, left, slices, slice_slabs;   // tiles: computed whole, and cut into slices
+    float us;
+};
+// The cheapest of the tile sizes and slicings by the costs above: whole tiles run in rounds of what the device holds; the last
+// round's, if they leave much of it idle, are cut along k instead.
 ProductPlan plan_product(int64_t M, int64_t N, int64_t K, int terms, int matrices) {
-    auto cut = [&](int b, int want) {
+    ProductPlan best = {};
+    best.us = INFINITY;
+    for (int c = kBig; c <= kMid; ++c) {
+        const TileCost& t = kTileCost[c];
         ProductPlan p = {};
-        p.big = b == 256;
-        p.tiles_m = (int)((M + b - 1) / b);
-        p.tiles_n = (int)((N + b - 1) / b);
-        const int64_t tiles = std::max<int64_t>(1, (int64_t)p.tiles_m * p.tiles_n * matrices), slabs = (K + kSlab - 1) / kSlab * terms;
-        int64_t s = std::min<int64_t>(kMaxSlices, std::max<int64_t>(1, std::min(want / tiles, slabs * kSlab / kMinSlice)));
-        p.slice_slabs = (int)std::max<int64_t>(1, (slabs + s - 1) / s);
-        p.slices = (int)std::max<int64_t>(1, (slabs + p.slice_slabs - 1) / p.slice_slabs);
-        return p;
-    };
-    const ProductPlan p = cut(256, kCus);
-    if ((int64_t)p.tiles_m * p.tiles_n * matrices * p.slices >= 3 * kCus / 4) return p;
-    return cut(128, 2 * kCus);
+        p.size = (TileSize)c;
+        p.tiles_m = (int)((M + t.m - 1) / t.m);
+        p.tiles_n = (int)((N + t.n - 1) / t.n);
+        const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * matrices, slots = (int64_t)kCus * t.per_cu;
+        const int64_t slabs = (K + t.slab - 1) / t.slab * terms;
+        const float each = (float)slabs * t.slab / 64 * t.us;
+        // a workgroup that has a compute unit to itself is not twice as fast as one of two
+        auto rounds = [&](int64_t groups, float us) {
+            if (t.per_cu == 2 && groups <= kCus) return 0.7f * us + kStartUs;
+            return (float)((groups + slots - 1) / slots) * (us + kStartUs);
+        };
+        for (int64_t s = 1; s <= kMaxSlices && (s == 1 || slabs * t.slab / s >= kMinSliceK); ++s) {
+            const int64_t over = s == 1 ? 0 : tiles % slots;
+            if (s > 1 && (over == 0 || over * s > slots)) break;
+            p.full = (int)(tiles - over);
+            p.left = (int)over;
+            p.slice_slabs = (int)std::max<int64_t>(1, (slabs + s - 1) / s);
+            p.slices = s == 1 ? 1 : (int)((slabs + p.slice_slabs - 1) / p.slice_slabs);
+            p.us = p.full ? rounds(p.full, each) : 0.f;
+            if (p.left) {
+                p.us += rounds((int64_t)p.left * p.slices, (float)p.slice_slabs * t.slab / 64 * t.us);
+                p.us += kSumUs + (float)((double)p.left * p.slices * t.m * t.n * 8 / kSumBytesPerUs);
+            }
+            if (p.us < best.us) best = p;
+        }
+    }
+    return best;
 }
-size_t part_bytes(const ProductPlan& p, int64_t M, int64_t N, int matrices) {
-    return p.slices > 1 ? align256((size_t)p.slices * matrices * M * N * 4) : 0;
+size_t part_bytes(const ProductPlan& p) {
+    return p.slices > 1 ? align256((size_t)p.left * p.slices * kTileCost[p.size].m * kTileCost[p.size].n * 4) : 0;
 }
 
-template <bool AK, bool BK, typename T>
-int launch_product(ProductArgs& g, const ProductPlan& p, void* part, hipStream_t st) {
-    g.tiles_m = p.tiles_m; g.tiles_n = p.tiles_n; g.slices = p.slices; g.slice_slabs = p.slice_slabs;
-    g.part = static_cast<float*>(part);
-    const dim3 grid((unsigned)((int64_t)p.tiles_m * p.tiles_n * g.matrices), (unsigned)p.slices);
-    using Big = Tile<256, 256, 2, 4, AK, BK, false>;
-    using Mid = Tile<128, 128, 2, 2, AK, BK, false>;
-    if (p.big) BPT_LAUNCH("product_kernel", (product_kernel<Big, 256, 256, AK, BK, T>), grid, dim3(Big::kThreads), 0, st, g);
-    else BPT_LAUNCH("product_kernel", (product_kernel<Mid, 128, 128, AK, BK, T>), grid, dim3(Mid::kThreads), 0, st, g);
+template <typename C, bool AK, bool BK, typename T>
+int launch_product(const ProductArgs& g, int left, hipStream_t st) {
+    BPT_LAUNCH("product_kernel", (product_kernel<C, AK, BK, T>), dim3((unsigned)(g.full + left * g.slices)), dim3(C::kThreads), 0, st, g);
     BPT_HIP(hipGetLastError());
-    if (p.slices > 1) {
-        const int64_t elems = g.M * g.N;
-        BPT_LAUNCH("product_sum_kernel", product_sum_kernel<T>, dim3((unsigned)((elems / 4 + 255) / 256), (unsigned)g.matrices), dim3(256), 0,
-                   st, g.part, p.slices, elems, g.N, g.ldc, static_cast<T*>(g.C[0]), static_cast<T*>(g.C[1]));
+    if (g.slices > 1) {
+        BPT_LAUNCH("product_sum_kernel", (product_sum_kernel<C, T>), dim3((unsigned)left, C::kBlocks), dim3(C::kThreads), 0, st, g);
         BPT_HIP(hipGetLastError());
     }
     return BPT_OK;
 }
+template <bool AK, bool BK, typename T>
+int launch_product(ProductArgs& g, const ProductPlan& p, void* part, hipStream_t st) {
+    g.tiles_m = p.tiles_m; g.tiles_n = p.tiles_n; g.full = p.full; g.slices = p.slices; g.slice_slabs = p.slice_slabs;
+    g.part = static_cast<float4*>(part);
+    if (p.size == kBig) return launch_product<Tile<256, 256, 2, 4, 64, 2, AK, BK, false>, AK, BK, T>(g, p.left, st);
+    if (p.size == kWide) return launch_product<Tile<128, 256, 1, 4, 32, 3, AK, BK, false>, AK, BK, T>(g, p.left, st);
+    return launch_product<Tile<128, 128, 2, 2, 64, 2, AK, BK, false>, AK, BK, T>(g, p.left, st);
+}
+
+// Tiles of the hidden activations, 128 rows by 128 columns of both halves or, where these leave compute units idle, by 64
+bool wide_hidden(int64_t M, int f) { return ((M + 127) / 128) * ((f + 127) / 128) >= kCus; }
 
 template <int ACT>
 int launch_up(UpArgs& g, hipStream_t st) {
-    const int64_t big = ((g.M + 255) / 256) * ((g.f + 127) / 128);
-    const bool is_big = big >= 3 * kCus / 4;
-    const int bm = is_big ? 256 : 128, bn = is_big ? 128 : 64;
-    g.tiles_m = (int)((g.M + bm - 1) / bm);
-    g.tiles_n = (g.f + bn - 1) / bn;
+    const bool wide = wide_hidden(g.M, g.f);
+    g.tiles_m = (int)((g.M + 127) / 128);
+    g.tiles_n = wide ? (g.f + 127) / 128 : (g.f + 63) / 64;
     const dim3 grid((unsigned)((int64_t)g.tiles_m * g.tiles_n));
-    using Big = Tile<256, 256, 2, 4, true, false, true>;
-    using Mid = Tile<128, 128, 2, 2, true, false, true>;
-    if (is_big) BPT_LAUNCH("gated_up_kernel", (gated_up_kernel<Big, 256, 256, ACT>), grid, dim3(Big::kThreads), 0, st, g);
-    else BPT_LAUNCH("gated_up_kernel", (gated_up_kernel<Mid, 128, 128, ACT>), grid, dim3(Mid::kThreads), 0, st, g);
+    using Wide = Tile<128, 256, 2, 2, 32, 3, true, false, true>;
+    using Mid = Tile<128, 128, 2, 2, 64, 2, true, false, true>;
+    if (wide) BPT_LAUNCH("gated_up_kernel", (gated_up_kernel<Wide, ACT>), grid, dim3(Wide::kThreads), 0, st, g);
+    else BPT_LAUNCH("gated_up_kernel", (gated_up_kernel<Mid, ACT>), grid, dim3(Mid::kThreads), 0, st, g);
     BPT_HIP(hipGetLastError());
     return BPT_OK;
 }
 
 template <int ACT>
 int launch_hidden(HiddenArgs& g, hipStream_t st) {
-    const int64_t big = ((g.M + 255) / 256) * ((g.f + 127) / 128);
-    const bool is_big = big >= 3 * kCus / 4;
-    const int bm = is_big ? 256 : 128, bn = is_big ? 128 : 64;
-    g.tiles_m = (int)((g.M + bm - 1) / bm);
-    g.tiles_n = (g.f + bn - 1) / bn;
+    const bool wide = wide_hidden(g.M, g.f);
+    g.tiles_m = (int)((g.M + 127) / 128);
+    g.tiles_n = wide ? (g.f + 127) / 128 : (g.f + 63) / 64;
     const dim3 grid((unsigned)((int64_t)g.tiles_m * g.tiles_n));
-    using Big = Tile<256, 256, 2, 4, true, false, true>;
-    using Big2 = Tile<256, 128, 2, 4, true, true, false>;
-    using Mid = Tile<128, 128, 2, 2, true, false, true>;
-    using Mid2 = Tile<128, 64, 2, 2, true, true, false>;
-    if (is_big) BPT_LAUNCH("gated_hidden_bwd_kernel", (gated_hidden_bwd_kernel<Big, Big2, 256, 256, ACT>), grid, dim3(Big::kThreads), 0, st, g);
-    else BPT_LAUNCH("gated_hidden_bwd_kernel", (gated_hidden_bwd_kernel<Mid, Mid2, 128, 128, ACT>), grid, dim3(Mid::kThreads), 0, st, g);
+    using Wide = Tile<128, 256, 1, 4, 32, 3, true, false, true>;
+    using Wide2 = Tile<128, 128, 1, 4, 32, 3, true, true, false>;
+    using Mid = Tile<128, 128, 2, 2, 64, 2, true, false, true>;
+    using Mid2 = Tile<128, 64, 2, 2, 64, 2, true, true, false>;
+    if (wide) BPT_LAUNCH("gated_hidden_bwd_kernel", (gated_hidden_bwd_kernel<Wide, Wide2, ACT>), grid, dim3(Wide::kThreads), 0, st, g);
+    else BPT_LAUNCH("gated_hidden_bwd_kernel", (gated_hidden_bwd_kernel<Mid, Mid2, ACT>), grid, dim3(Mid::kThreads), 0, st, g);
     BPT_HIP(hipGetLastError());
     return BPT_OK;
 }
@@ -332,7 +427,7 @@ FwdBuffers fwd_buffers(const bpt_gated_ffn_t* s) {
     b.down = plan_product(s->rows, s->d, s->f, 1, 1);
     b.F = 0;
     b.part = align256((size_t)s->rows * s->f * 2);
-    b.total = b.part + part_bytes(b.down, s->rows, s->d, 1);
+    b.total = b.part + part_bytes(b.down);
     return b;
 }
 struct BwdBuffers {
@@ -349,7 +444,7 @@ BwdBuffers bwd_buffers(const bpt_gated_ffn_t* s) {
     b.dG = hidden;
     b.dU = 2 * hidden;
     b.part = 3 * hidden;
-    b.total = b.part + std::max(std::max(part_bytes(b.wd, s->f, s->d, 1), part_bytes(b.wgu, s->d, s->f, 2)), part_bytes(b.dx, s->rows, s->d, 1));
+    b.total = b.part + std::max(std::max(part_bytes(b.wd), part_bytes(b.wgu)), part_bytes(b.dx));
     return b;
 }
 

@@ -1,10 +1,10 @@
 // Tiles of a matrix product C[m][n] = sum_k A[m][k] B[k][n] on the matrix cores, for the feed-forward block: bf16 operands,
-// fp32 sums.  A workgroup computes BM x BN of C in WR x WC wavefronts; both operands go through LDS in slabs of 64 k,
-// two slabs deep, loaded straight into LDS (no registers in between).
+// fp32 sums.  A workgroup computes BM x BN of C in WR x WC wavefronts; both operands go through LDS in slabs of 32 or 64 k,
+// two or three slabs deep, loaded straight into LDS (no registers in between).
 //
 // An operand lies in memory with either k or its own index (m or n) contiguous, and is kept that way in LDS:
-//   k contiguous     [W][64]  128 bytes per row, read 16 bytes per lane (8 k of one row)
-//   index contiguous [64][W]  read with the transposing LDS reads, which hand a lane 4 k of one column
+//   k contiguous     [W][SLAB]  read 16 bytes per lane (8 k of one row)
+//   index contiguous [SLAB][W]  read with the transposing LDS reads, which hand a lane 4 k of one column
 // Either image is permuted within a row (16-byte pieces by the row's low bits, 32-byte pieces by the k's) so that the
 // lanes of one read fall into different banks; direct loads write LDS in lane order, so the permutation is applied to
 // the addresses they read from.
@@ -20,11 +20,28 @@ namespace {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef int i32x2_t __attribute__((ext_vector_type(2)));
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
 typedef short i16x4_t __attribute__((ext_vector_type(4)));
 typedef short i16x8_t __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) unsigned char* lds_bytes_t;
 
-constexpr int kSlab = 64;                       // k per slab
+// 16 bytes per lane from the buffer `r` at byte offset `off` straight to LDS, lane after lane from `to` on.  Written out
+// because the compiler waits for such a load before any LDS read behind it, whatever the two touch; who reads the slab waits
+// with slab_barrier.  (M0 holds the LDS address; a wait state lies between its write and its use.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"   // (M0 as a clobber: it is the compiler's own, set right before each use)
+__device__ __forceinline__ void load_to_lds(i32x4_t r, int off, lds_bytes_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 :: "s"((int)(uintptr_t)to), "v"(off), "s"(r) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+// All but the last PENDING loads of this wavefront have arrived, its LDS reads are through, and so are those of the others
+template <int PENDING>
+__device__ __forceinline__ void slab_barrier() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(PENDING) : "memory");
+}
+
 constexpr int kBound = 0x7FFFFFF0;              // bytes an operand's descriptor covers from its tile's first element
 constexpr int kOutside = (int)0x80000000;       // an offset behind it
 
@@ -35,10 +52,17 @@ __device__ __forceinline__ int piece_swap(int k) {
     return W >= 128 ? 2 * (k & 3) : W == 64 ? (k & 3) : (k & 1);
 }
 
+// the same for the 16-byte pieces of a row of SLAB k (k contiguous): 16 neighbouring rows, read at once, fall into the 16
+// different pieces of 256 bytes (the banks' width)
+template <int SLAB>
+__device__ __forceinline__ int row_swap(int row) {
+    return SLAB == 64 ? ((row >> 1) & 7) : ((row >> 2) & 3);
+}
+
 // Loads a slab of an operand of W rows (or columns) into LDS with WAVES wavefronts.
-template <int W, int WAVES, bool KFIRST>   // KFIRST: k contiguous
+template <int W, int WAVES, bool KFIRST, int SLAB>   // KFIRST: k contiguous
 struct SlabLoader {
-    static constexpr int kBytes = W * kSlab * 2;
+    static constexpr int kBytes = W * SLAB * 2;
     static constexpr int kLoads = kBytes / 1024 / WAVES;   // 1 KB per wavefront and instruction
     static_assert(kLoads * 1024 * WAVES == kBytes, "the wavefronts share the slab evenly");
     int off[kLoads];
@@ -47,8 +71,9 @@ struct SlabLoader {
     static __device__ __forceinline__ void place(int i, int wave, int lane, int& index, int& k) {
         const int q = (i * WAVES + wave) * 64 + lane;
         if (KFIRST) {
-            index = q >> 3;
-            k = ((q & 7) ^ (index & 7)) * 8;
+            constexpr int kPieces = SLAB / 8;
+            index = q / kPieces;
+            k = ((q % kPieces) ^ row_swap<SLAB>(index)) * 8;
         } else {
             constexpr int kPieces = W / 8;
             k = q / kPieces;
@@ -68,29 +93,28 @@ struct SlabLoader {
     }
     // p: the tile's first element of this slab; k_left: k that exist from there on
     __device__ __forceinline__ void load(const bf16_t* p, int64_t k_left, lds_bytes_t lds, int wave, int lane) const {
-        __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(p), 0, kBound, 0x00020000);
-        if (k_left >= kSlab) {
+        const uint64_t at = reinterpret_cast<uint64_t>(p);
+        const i32x4_t r = {__builtin_amdgcn_readfirstlane((int)at), __builtin_amdgcn_readfirstlane((int)(at >> 32) & 0xFFFF), kBound, 0x00020000};
+        if (k_left >= SLAB) {
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + (i * WAVES + wave) * 1024), 16, off[i], 0, 0, 0);
+            for (int i = 0; i < kLoads; ++i) load_to_lds(r, off[i], lds + (i * WAVES + wave) * 1024);
         } else {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 int index, k;
                 place(i, wave, lane, index, k);
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + (i * WAVES + wave) * 1024), 16,
-                                                         k < k_left ? off[i] : kOutside, 0, 0, 0);
+                load_to_lds(r, k < k_left ? off[i] : kOutside, lds + (i * WAVES + wave) * 1024);
             }
         }
     }
 };
 
 // Operand of v_mfma_f32_32x32x16_bf16: lane l holds k = 16 kk + 8 (l / 32) .. + 7 of index first + l % 32.
-template <int W, bool KFIRST>
+template <int W, bool KFIRST, int SLAB>
 __device__ __forceinline__ bf16x8_t fragment(lds_bytes_t slab, int first, int kk, int lane) {
     if constexpr (KFIRST) {
         typedef __attribute__((address_space(3))) const bf16x8_t* ptr_t;
-        return *(ptr_t)(slab + (first + (lane & 31)) * 128 + (((kk * 2 + (lane >> 5)) ^ (lane & 7)) * 16));
+        return *(ptr_t)(slab + (first + (lane & 31)) * (SLAB * 2) + (((kk * 2 + (lane >> 5)) ^ row_swap<SLAB>(lane & 31)) * 16));
     } else {
         typedef __attribute__((address_space(3))) i16x4_t* ptr_t;
         const int k = kk * 16 + (lane >> 5) * 8 + ((lane & 15) >> 2);
@@ -105,16 +129,20 @@ __device__ __forceinline__ bf16x8_t fragment(lds_bytes_t slab, int first, int kk
 
 // One operand pair of a tile.  PAIR: B is two matrices of BN / 2 columns each, whose slabs lie one behind the other; a
 // wavefront then computes the same columns of both (the first half of its column blocks are of the first).
-template <int BM, int BN, int WR, int WC, bool A_KFIRST, bool B_KFIRST, bool PAIR>
+template <int BM, int BN, int WR, int WC, int SLAB, int STAGES, bool A_KFIRST, bool B_KFIRST, bool PAIR>
 struct Tile {
+    static constexpr int kSlab = SLAB;                         // k per slab
     static constexpr int kWaves = WR * WC, kThreads = 64 * kWaves;
     static constexpr int kRows = BM / WR / 32;                 // 32-row blocks of a wavefront
     static constexpr int kCols = BN / WC / 32;                 // 32-column blocks
+    static constexpr int kBlocks = kRows * kCols;
+    static constexpr int kBM = BM, kBN = BN;
     static constexpr int kBWidth = PAIR ? BN / 2 : BN;
-    using LoadA = SlabLoader<BM, kWaves, A_KFIRST>;
-    using LoadB = SlabLoader<kBWidth, kWaves, B_KFIRST>;
+    using LoadA = SlabLoader<BM, kWaves, A_KFIRST, SLAB>;
+    using LoadB = SlabLoader<kBWidth, kWaves, B_KFIRST, SLAB>;
     static constexpr int kStage = LoadA::kBytes + LoadB::kBytes * (PAIR ? 2 : 1);
-    static constexpr int kLds = 2 * kStage;
+    static constexpr int kLds = STAGES * kStage;
+    static constexpr int kPending = (LoadA::kLoads + LoadB::kLoads * (PAIR ? 2 : 1));   // loads of a slab, per wavefront
     typedef f32x16_t Acc[kRows][kCols];
 
     LoadA la;
@@ -123,17 +151,21 @@ struct Tile {
     int wave, lane, wr, wc;
 
     __device__ __forceinline__ void init(unsigned char* shared, int64_t lda, int64_t rows_valid, int64_t ldb, int64_t cols_valid) {
+        place(shared);
+        la.init(wave, lane, lda, rows_valid);
+        lb.init(wave, lane, ldb, cols_valid);
+    }
+    __device__ __forceinline__ void place(unsigned char* shared) {
         lds = (lds_bytes_t)shared;
         lane = threadIdx.x & 63;
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         wr = wave / WC;
         wc = wave % WC;
-        la.init(wave, lane, lda, rows_valid);
-        lb.init(wave, lane, ldb, cols_valid);
     }
     // first column, within the tile's BN (PAIR: within either half), of a column block of this wavefront
     __device__ __forceinline__ int col_of(int j) const {
-        return PAIR ? (wc * (kCols / 2) + j % (kCols / 2)) * 32 : (wc * kCols + j) * 32;
+        if constexpr (PAIR) return (wc * (kCols / 2) + j % (kCols / 2)) * 32;
+        return (wc * kCols + j) * 32;
     }
     __device__ __forceinline__ int row_of(int i) const { return (wr * kRows + i) * 32; }
 
@@ -151,10 +183,10 @@ struct Tile {
 #pragma unroll
             for (int j = 0; j < kCols; ++j) {
                 lds_bytes_t p = PAIR && j >= kCols / 2 ? pb + LoadB::kBytes : pb;
-                b[j] = fragment<kBWidth, B_KFIRST>(p, col_of(j), kk, lane);
+                b[j] = fragment<kBWidth, B_KFIRST, SLAB>(p, col_of(j), kk, lane);
             }
 #pragma unroll
-            for (int i = 0; i < kRows; ++i) a[i] = fragment<BM, A_KFIRST>(pa, row_of(i), kk, lane);
+            for (int i = 0; i < kRows; ++i) a[i] = fragment<BM, A_KFIRST, SLAB>(pa, row_of(i), kk, lane);
 #pragma unroll
             for (int i = 0; i < kRows; ++i)
 #pragma unroll
@@ -162,26 +194,60 @@ struct Tile {
         }
     }
     // Sum over `slabs` slabs; from(t, a, b0, b1, k_left) says where slab t lies.  All threads call it; on return the
-    // slabs' memory is free.
+    // slabs' memory is free.  STAGES - 1 slabs are on their way while one is worked on, one barrier per slab.
     template <typename From>
     __device__ __forceinline__ void run(Acc& acc, int slabs, From from) const {
         const bf16_t *a, *b0, *b1 = nullptr;
         int64_t k_left;
-        if (slabs > 0) {
-            from(0, a, b0, b1, k_left);
-            load(a, b0, b1, k_left, 0);
-        }
-        __syncthreads();
-        for (int t = 0; t < slabs; ++t) {
-            if (t + 1 < slabs) {
-                from(t + 1, a, b0, b1, k_left);
-                load(a, b0, b1, k_left, (t + 1) & 1);
+#pragma unroll
+        for (int t = 0; t < STAGES - 1; ++t)
+            if (t < slabs) {
+                from(t, a, b0, b1, k_left);
+                load(a, b0, b1, k_left, t);
             }
-            multiply(acc, t & 1);
-            __syncthreads();
+        int stage = 0, next = STAGES - 1;
+        for (int t = 0; t < slabs; ++t) {
+            if (STAGES == 2 || t + 1 == slabs) slab_barrier<0>();
+            else slab_barrier<kPending * (STAGES - 2)>();
+            if (t + STAGES - 1 < slabs) {
+                from(t + STAGES - 1, a, b0, b1, k_left);
+                load(a, b0, b1, k_left, next);
+            }
+            multiply(acc, stage);
+            stage = stage + 1 == STAGES ? 0 : stage + 1;
+            next = next + 1 == STAGES ? 0 : next + 1;
+        }
+        slab_barrier<0>();
+    }
+};
+// Rounds 32 rows of a wavefront's COLS columns to bf16 and writes them, through LDS of its own, in 16-byte pieces along the
+// rows (from the accumulators' order a store would touch 32 rows for 16 bytes each).  A wavefront's LDS accesses are in
+// order, so nothing is waited for between blocks of rows.
+template <int COLS>
+struct RowBlock {
+    static constexpr int kPitch = COLS * 2 + 16, kBytes = 32 * kPitch;
+    lds_bytes_t lds;
+    int lane;
+    __device__ __forceinline__ RowBlock(lds_bytes_t all, int wave, int lane_) : lds(all + wave * kBytes), lane(lane_) {}
+    // four neighbours of row lane % 32: columns col + 4 (lane / 32) ..
+    __device__ __forceinline__ void put(int col, float a, float b, float c, float d) const {
+        typedef __attribute__((address_space(3))) i32x2_t* ptr_t;
+        const i32x2_t v = {(int)bf16_pair(a, b), (int)bf16_pair(c, d)};
+        *(ptr_t)(lds + (lane & 31) * kPitch + (col + 4 * (lane >> 5)) * 2) = v;
+    }
+    // out: the block's first element; rows, cols: how many of them exist
+    __device__ __forceinline__ void write(bf16_t* out, int64_t ld, int64_t rows, int cols) const {
+        typedef __attribute__((address_space(3))) const i32x4_t* ptr_t;
+        constexpr int kPieces = COLS / 8, kRows = 64 / kPieces;
+        const int r = lane / kPieces, c = lane % kPieces * 8;
+#pragma unroll
+        for (int i = 0; i < 32; i += kRows) {
+            const i32x4_t v = *(ptr_t)(lds + (i + r) * kPitch + c * 2);
+            if (i + r < rows && c < cols) *reinterpret_cast<i32x4_t*>(out + (i + r) * ld + c) = v;
         }
     }
 };
+
 // acc[i][j] register r of lane l is C[row_of(i) + l % 32][col_of(j) + 8 (r / 4) + 4 (l / 32) + r % 4]: the matrix
 // instruction is given B as its first operand, so that a lane holds four neighbours of a row of C.
 
