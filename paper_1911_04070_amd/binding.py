@@ -708,6 +708,10 @@ NORMS = {"none": 0, "layer": 1, "rms": 2}
 ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}
 
 
+# the current stream's handle without a Stream object around it, which costs a small call more than its kernel
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: int(torch.cuda.current_stream(index).cuda_stream))
+
+
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
@@ -759,7 +763,7 @@ def bpt_rotary(Q: torch.Tensor, K: Optional[torch.Tensor], pos: torch.Tensor, ro
     shp = BptRotary(B, H, N, D, dt, s[0], s[1], s[2], o[0], o[1], o[2], D if rot is None else int(rot), bool(interleaved), bool(inverse),
                     base, factor, context, low, high)
     _check(load_library().bpt_rotary(ctypes.byref(shp), pos.data_ptr(), pos.stride(0) if pos.dim() == 2 else 0, Q.data_ptr(), _ptr(K),
-                                     Qr.data_ptr(), _ptr(Kr), _stream_ptr()), "bpt_rotary")
+                                     Qr.data_ptr(), _ptr(Kr), _raw_stream(dev.index)), "bpt_rotary")
     return Qr, Kr
 
 
@@ -824,7 +828,7 @@ def bpt_residual_norm_fwd(x: torch.Tensor, branch: Optional[torch.Tensor], gate:
     h = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device) if s.pre else None
     stats = torch.empty((s.rows, 4), dtype=torch.float32, device=x.device) if want_stats else None
     _check(load_library().bpt_residual_norm_fwd(ctypes.byref(s), x.data_ptr(), _ptr(branch), _ptr(gate), _ptr(post_gain), _ptr(post_bias),
-                                                _ptr(pre_gain), _ptr(pre_bias), y.data_ptr(), _ptr(h), _ptr(stats), _stream_ptr()),
+                                                _ptr(pre_gain), _ptr(pre_bias), y.data_ptr(), _ptr(h), _ptr(stats), _raw_stream(x.device.index)),
            "bpt_residual_norm_fwd")
     return (y, h, stats) if want_stats else (y, h)
 
@@ -857,7 +861,7 @@ def bpt_residual_norm_bwd(x: torch.Tensor, branch: Optional[torch.Tensor], gate:
     ws, ws_ptr = _workspace(need, x.device)
     _check(L.bpt_residual_norm_bwd(ctypes.byref(s), x.data_ptr(), _ptr(branch), _ptr(gate), _ptr(post_gain), _ptr(post_bias),
                                    _ptr(pre_gain), _ptr(pre_bias), stats.data_ptr(), _ptr(dy), _ptr(dh), out["dx"].data_ptr(),
-                                   _ptr(out.get("d_branch")), ctypes.byref(grads), ws_ptr, need, _stream_ptr()),
+                                   _ptr(out.get("d_branch")), ctypes.byref(grads), ws_ptr, need, _raw_stream(x.device.index)),
            "bpt_residual_norm_bwd")
     return out
 
@@ -890,7 +894,7 @@ def bpt_gated_ffn_fwd(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: t
     if workspace is None:
         workspace = torch.empty(need, dtype=torch.uint8, device=X.device)
     _check(L.bpt_gated_ffn_fwd(ctypes.byref(s), X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(), out.data_ptr(),
-                               workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_ptr()), "bpt_gated_ffn_fwd")
+                               workspace.data_ptr(), workspace.numel() * workspace.element_size(), _raw_stream(X.device.index)), "bpt_gated_ffn_fwd")
     return out
 
 
@@ -908,7 +912,7 @@ def bpt_gated_ffn_bwd(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: t
         workspace = torch.empty(need, dtype=torch.uint8, device=X.device)
     _check(L.bpt_gated_ffn_bwd(ctypes.byref(s), X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(), dY.data_ptr(), dX.data_ptr(),
                                dWg.data_ptr(), dWu.data_ptr(), dWd.data_ptr(), workspace.data_ptr(),
-                               workspace.numel() * workspace.element_size(), _stream_ptr()), "bpt_gated_ffn_bwd")
+                               workspace.numel() * workspace.element_size(), _raw_stream(X.device.index)), "bpt_gated_ffn_bwd")
     return dX, dWg, dWu, dWd
 
 

@@ -19,9 +19,23 @@ __device__ __forceinline__ void activation(float g, float& value, float& slope) 
         value = g * s;
         slope = s * (1.f + g * (1.f - s));
     } else if constexpr (ACT == BPT_ACT_GELU) {
-        const float s = 0.5f * (1.f + erff(g * 0.70710678118654752f));
+        // Phi(-|g|) = exp(-g^2 / 2) t q(t), t = 1 / (1 + 0.3 |g|): q is a polynomial of degree 7 fitted (least squares, weights
+        // moved to level the error) to the scaled complementary error function over |g| <= 14, 1.5e-7 relative; with fp32
+        // arithmetic 2e-6 relative for |g| <= 6, where erff and the exponential of the slope would cost twice the instructions
+        const float e = __builtin_amdgcn_exp2f(g * g * -0.72134752044448170f);
+        const float t = __builtin_amdgcn_rcpf(fmaf(0.3f, fabsf(g), 1.f));
+        float q = 0.035674779f;
+        q = fmaf(q, t, -0.157203101f);
+        q = fmaf(q, t, 0.206353537f);
+        q = fmaf(q, t, -0.053683671f);
+        q = fmaf(q, t, 0.128561640f);
+        q = fmaf(q, t, 0.099913488f);
+        q = fmaf(q, t, 0.120753957f);
+        q = fmaf(q, t, 0.119629299f);
+        const float below = q * t * e;
+        const float s = g > 0.f ? 1.f - below : below;
         value = g * s;
-        slope = s + g * 0.39894228040143268f * __expf(-0.5f * g * g);
+        slope = s + g * 0.39894228040143268f * e;
     } else {
         value = g <= 0.f ? 0.f : g;   // (a NaN stays one)
         slope = g <= 0.f ? 0.f : 1.f;
@@ -53,7 +67,7 @@ struct UpArgs {
     int32_t d, f, tiles_m, tiles_n;
 };
 template <typename C, int ACT>
-__global__ void __launch_bounds__(C::kThreads, 2) gated_up_kernel(const UpArgs g) {
+__global__ void __launch_bounds__(C::kThreads, C::kWavesPerSimd) gated_up_kernel(const UpArgs g) {
     __shared__ __attribute__((aligned(1024))) unsigned char shared[C::kLds];
     int tm, tn;
     tile_of(blockIdx.x, g.tiles_m, g.tiles_n, tm, tn);
@@ -92,6 +106,57 @@ __global__ void __launch_bounds__(C::kThreads, 2) gated_up_kernel(const UpArgs g
     }
 }
 
+// ---- few rows ---------------------------------------------------------------------------------------------------
+// Neighbouring strips of 32 columns share cache lines, so an XCD gets a run of them.
+__device__ __forceinline__ int strip_of(int id, int strips) {
+    const int each = strips / kXcds, more = strips % kXcds, xcd = id % kXcds;
+    return xcd * each + min(xcd, more) + id / kXcds;
+}
+using UpStrip = Strip<4, 4, true>;
+template <int ACT>
+__global__ void __launch_bounds__(UpStrip::kThreads) gated_up_strip_kernel(const UpArgs g) {
+    __shared__ __attribute__((aligned(1024))) unsigned char shared[UpStrip::kLds];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n0 = strip_of(blockIdx.x, gridDim.x) * 32;
+    const int64_t m0 = (int64_t)blockIdx.y * 32;
+    const bf16_t* w[2] = {g.Wg + n0, g.Wu + n0};
+    float4 sum[2];
+    UpStrip::run(shared, wave, lane, g.X + m0 * g.ldx, g.ldx, g.M - m0, w, g.f, g.f - n0, 0, g.d, sum);
+    const int64_t m = m0 + (lane & 31);
+    const int n = n0 + 8 * wave + 4 * (lane >> 5);
+    if (wave >= 4 || m >= g.M || n >= g.f) return;
+    const float gate[4] = {sum[0].x, sum[0].y, sum[0].z, sum[0].w}, up[4] = {sum[1].x, sum[1].y, sum[1].z, sum[1].w};
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        float value, slope;
+        activation<ACT>(gate[e], value, slope);
+        v[e] = value * up[e];
+    }
+    *reinterpret_cast<uint2*>(g.F + m * g.f + n) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+}
+
+struct DownArgs {
+    const bf16_t *F, *Wd;
+    bf16_t* Y;
+    int64_t M, ldy;
+    int32_t d, f;
+};
+using DownStrip = Strip<8, 4, false>;
+__global__ void __launch_bounds__(DownStrip::kThreads) down_strip_kernel(const DownArgs g) {
+    __shared__ __attribute__((aligned(1024))) unsigned char shared[DownStrip::kLds];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n0 = strip_of(blockIdx.x, gridDim.x) * 32;
+    const int64_t m0 = (int64_t)blockIdx.y * 32;
+    const bf16_t* w[1] = {g.Wd + n0};
+    float4 sum[1];
+    DownStrip::run(shared, wave, lane, g.F + m0 * g.f, g.f, g.M - m0, w, g.d, g.d - n0, 0, g.f, sum);
+    const int64_t m = m0 + (lane & 31);
+    const int n = n0 + 8 * wave + 4 * (lane >> 5);
+    if (wave >= 4 || m >= g.M || n >= g.d) return;
+    *reinterpret_cast<uint2*>(g.Y + m * g.ldy + n) = make_uint2(bf16_pair(sum[0].x, sum[0].y), bf16_pair(sum[0].z, sum[0].w));
+}
+
 // ---- C = A0 B0 (+ A1 B1), or several products side by side ------------------------------------------------------
 // The first `full` tiles are computed whole; what is left over is less than the device holds at once and is cut into
 // `slices` of k, whose sums go to `part` and are added by product_sum_kernel, in order.
@@ -117,7 +182,7 @@ __device__ __forceinline__ ProductTile product_tile(const ProductArgs& g, int id
     return {mat, (tn - mat * g.tiles_n) * C::kBN, (int64_t)tm * C::kBM};
 }
 template <typename C, bool A_KFIRST, bool B_KFIRST, typename T>
-__global__ void __launch_bounds__(C::kThreads, 2) product_kernel(const ProductArgs g) {
+__global__ void __launch_bounds__(C::kThreads, C::kWavesPerSimd) product_kernel(const ProductArgs g) {
     __shared__ __attribute__((aligned(1024))) unsigned char shared[C::kLds];
     const int over = max((int)blockIdx.x - g.full, 0), slice = (int)blockIdx.x < g.full ? 0 : over % g.slices;
     const bool whole = (int)blockIdx.x < g.full || g.slices == 1;
@@ -225,7 +290,7 @@ struct HiddenArgs {
 };
 // G = X Wg and U = X Wu are formed again, then dF = dY Wd^T on the same tile: F, dG and dU are written, rounded once.
 template <typename C, typename C2, int ACT>
-__global__ void __launch_bounds__(C::kThreads, 2) gated_hidden_bwd_kernel(const HiddenArgs g) {
+__global__ void __launch_bounds__(C::kThreads, C::kWavesPerSimd) gated_hidden_bwd_kernel(const HiddenArgs g) {
     __shared__ __attribute__((aligned(1024))) unsigned char shared[C::kLds > C2::kLds ? C::kLds : C2::kLds];
     int tm, tn;
     tile_of(blockIdx.x, g.tiles_m, g.tiles_n, tm, tn);
@@ -273,6 +338,7 @@ __global__ void __launch_bounds__(C::kThreads, 2) gated_hidden_bwd_kernel(const 
                     v[e] = value * up;
                     gu[i][j][4 * q + e] = value;
                     gu[i][kHalf + j][4 * q + e] = up * slope;
+                    if (e & 1) __builtin_amdgcn_sched_barrier(0);   // (192 sums are in registers: few activations at a time)
                 }
                 block.put(j * 32 + 8 * q, v[0], v[1], v[2], v[3]);
             }
@@ -298,15 +364,16 @@ constexpr int kCus = 256;
 
 // Sizes of a workgroup's tile.  kBig: 256 x 256, slabs of 64, one workgroup of 8 wavefronts per compute unit; kWide: 128 x 256,
 // slabs of 32, three deep, and kMid: 128 x 128, slabs of 64: two workgroups of 4 wavefronts per compute unit, of which
-// one multiplies while the other starts up or writes.
-enum TileSize { kBig, kWide, kMid };
+// one multiplies while the other starts up or writes; kSmall: 64 x 64, slabs of 64, four deep: for products of few tiles, whose
+// time is the slabs' latency.  Times measured on all four products of the block (both operands' orders differ by 10 %).
+enum TileSize { kBig, kWide, kMid, kSmall };
 struct TileCost {
     int m, n, slab, per_cu;
-    float us;        // of 64 k, all compute units busy
+    float us, us_alone;   // of 64 k, all compute units busy; and with at most one workgroup on each
 };
-constexpr TileCost kTileCost[] = {{256, 256, 64, 1, 2.1f}, {128, 256, 32, 2, 2.35f}, {128, 128, 64, 2, 1.25f}};
-constexpr float kStartUs = 3.f;              // a tile's first loads and its results
-constexpr float kSumUs = 5.f, kSumBytesPerUs = 4.0e6f;   // adding up slices: a launch, and their bytes written and read
+constexpr TileCost kTileCost[] = {{256, 256, 64, 1, 2.1f, 2.1f}, {128, 256, 32, 2, 2.35f, 1.5f}, {128, 128, 64, 2, 1.25f, 0.68f}, {64, 64, 64, 2, 0.53f, 0.40f}};
+constexpr float kStartUs = 2.5f;             // a tile's first loads and its results
+constexpr float kSumUs = 3.5f, kSumBytesPerUs = 5.0e6f;   // adding up slices: a launch, and their bytes written and read
 constexpr int kMaxSlices = 32, kMinSliceK = 128;
 
 struct ProductPlan {
@@ -319,7 +386,7 @@ struct ProductPlan {
 ProductPlan plan_product(int64_t M, int64_t N, int64_t K, int terms, int matrices) {
     ProductPlan best = {};
     best.us = INFINITY;
-    for (int c = kBig; c <= kMid; ++c) {
+    for (int c = kBig; c <= kSmall; ++c) {
         const TileCost& t = kTileCost[c];
         ProductPlan p = {};
         p.size = (TileSize)c;
@@ -327,11 +394,10 @@ ProductPlan plan_product(int64_t M, int64_t N, int64_t K, int terms, int matrice
         p.tiles_n = (int)((N + t.n - 1) / t.n);
         const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * matrices, slots = (int64_t)kCus * t.per_cu;
         const int64_t slabs = (K + t.slab - 1) / t.slab * terms;
-        const float each = (float)slabs * t.slab / 64 * t.us;
-        // a workgroup that has a compute unit to itself is not twice as fast as one of two
-        auto rounds = [&](int64_t groups, float us) {
-            if (t.per_cu == 2 && groups <= kCus) return 0.7f * us + kStartUs;
-            return (float)((groups + slots - 1) / slots) * (us + kStartUs);
+        auto rounds = [&](int64_t groups, int64_t n) {   // of workgroups with n slabs each
+            const float k = (float)n * t.slab / 64;
+            if (groups <= kCus) return k * t.us_alone + kStartUs;
+            return (float)((groups + slots - 1) / slots) * (k * t.us + kStartUs);
         };
         for (int64_t s = 1; s <= kMaxSlices && (s == 1 || slabs * t.slab / s >= kMinSliceK); ++s) {
             const int64_t over = s == 1 ? 0 : tiles % slots;
@@ -340,9 +406,9 @@ ProductPlan plan_product(int64_t M, int64_t N, int64_t K, int terms, int matrice
             p.left = (int)over;
             p.slice_slabs = (int)std::max<int64_t>(1, (slabs + s - 1) / s);
             p.slices = s == 1 ? 1 : (int)((slabs + p.slice_slabs - 1) / p.slice_slabs);
-            p.us = p.full ? rounds(p.full, each) : 0.f;
+            p.us = p.full ? rounds(p.full, slabs) : 0.f;
             if (p.left) {
-                p.us += rounds((int64_t)p.left * p.slices, (float)p.slice_slabs * t.slab / 64 * t.us);
+                p.us += rounds((int64_t)p.left * p.slices, p.slice_slabs);
                 p.us += kSumUs + (float)((double)p.left * p.slices * t.m * t.n * 8 / kSumBytesPerUs);
             }
             if (p.us < best.us) best = p;
@@ -370,40 +436,70 @@ int launch_product(ProductArgs& g, const ProductPlan& p, void* part, hipStream_t
     g.part = static_cast<float4*>(part);
     if (p.size == kBig) return launch_product<Tile<256, 256, 2, 4, 64, 2, AK, BK, false>, AK, BK, T>(g, p.left, st);
     if (p.size == kWide) return launch_product<Tile<128, 256, 1, 4, 32, 3, AK, BK, false>, AK, BK, T>(g, p.left, st);
-    return launch_product<Tile<128, 128, 2, 2, 64, 2, AK, BK, false>, AK, BK, T>(g, p.left, st);
+    if (p.size == kMid) return launch_product<Tile<128, 128, 2, 2, 64, 2, AK, BK, false>, AK, BK, T>(g, p.left, st);
+    return launch_product<Tile<64, 64, 2, 2, 64, 4, AK, BK, false>, AK, BK, T>(g, p.left, st);
 }
 
-// Tiles of the hidden activations, 128 rows by 128 columns of both halves or, where these leave compute units idle, by 64
-bool wide_hidden(int64_t M, int f) { return ((M + 127) / 128) * ((f + 127) / 128) >= kCus; }
+// Strips of 32 x 32 serve as long as every one has a compute unit to itself (d = 512, f = 1368: 1 row, both products 6.7 + 9.9
+// -> 3.8 + 4.3 us; 128 rows 7.0 + 10.2 -> 4.3 + 4.6 us; d = 2048, f = 5464: 1 row 25 + 17 -> 10 + 8.5 us, 64 rows 26 + 16 ->
+// 24 + 12 us; with two per compute unit they are no faster than the tiles)
+bool use_strips(int64_t rows, int cols) { return ((rows + 31) / 32) * ((cols + 31) / 32) <= kCus; }
+dim3 strip_grid(int64_t rows, int cols) { return dim3((unsigned)((cols + 31) / 32), (unsigned)((rows + 31) / 32)); }
 
+// Tiles of the hidden activations: 128 rows by 128 columns of both halves, or by 64 where these leave compute units idle, or
+// 64 rows by 64 columns where those have a compute unit each (d = 512, f = 1368, 300 rows: 7.2 -> 6.0 us forward, 11.8 -> 9.5 us
+// backward; 1023 rows 7.6 -> 10.9 us, 13.6 -> 18.1 us); backward 256 rows by 128 columns for two rounds and more (65 532 rows,
+// d = 512, f = 2048: 573 -> 560 us; forward 309 -> 319 us, 9001 rows, d = 2048, f = 5464: 383 -> 392 us)
+enum HiddenSize { kHiddenBig, kHiddenWide, kHiddenMid, kHiddenSmall };
+HiddenSize hidden_tiles(int64_t M, int f, bool backward, int32_t& tiles_m, int32_t& tiles_n) {
+    auto count = [&](int m, int n) {
+        tiles_m = (int)((M + m - 1) / m);
+        tiles_n = (f + n - 1) / n;
+        return (int64_t)tiles_m * tiles_n;
+    };
+    if (count(64, 64) <= kCus) return kHiddenSmall;
+    if (backward && count(256, 128) >= 2 * kCus) return kHiddenBig;
+    if (count(128, 128) >= kCus) return kHiddenWide;
+    count(128, 64);
+    return kHiddenMid;
+}
+
+template <int ACT, typename C>
+int launch_up_as(const UpArgs& g, hipStream_t st) {
+    BPT_LAUNCH("gated_up_kernel", (gated_up_kernel<C, ACT>), dim3((unsigned)((int64_t)g.tiles_m * g.tiles_n)), dim3(C::kThreads), 0, st, g);
+    BPT_HIP(hipGetLastError());
+    return BPT_OK;
+}
 template <int ACT>
 int launch_up(UpArgs& g, hipStream_t st) {
-    const bool wide = wide_hidden(g.M, g.f);
-    g.tiles_m = (int)((g.M + 127) / 128);
-    g.tiles_n = wide ? (g.f + 127) / 128 : (g.f + 63) / 64;
-    const dim3 grid((unsigned)((int64_t)g.tiles_m * g.tiles_n));
-    using Wide = Tile<128, 256, 2, 2, 32, 3, true, false, true>;
-    using Mid = Tile<128, 128, 2, 2, 64, 2, true, false, true>;
-    if (wide) BPT_LAUNCH("gated_up_kernel", (gated_up_kernel<Wide, ACT>), grid, dim3(Wide::kThreads), 0, st, g);
-    else BPT_LAUNCH("gated_up_kernel", (gated_up_kernel<Mid, ACT>), grid, dim3(Mid::kThreads), 0, st, g);
+    if (use_strips(g.M, g.f)) {
+        BPT_LAUNCH("gated_up_strip_kernel", gated_up_strip_kernel<ACT>, strip_grid(g.M, g.f), dim3(UpStrip::kThreads), 0, st, g);
+        BPT_HIP(hipGetLastError());
+        return BPT_OK;
+    }
+    const HiddenSize size = hidden_tiles(g.M, g.f, false, g.tiles_m, g.tiles_n);
+    if (size == kHiddenWide) return launch_up_as<ACT, Tile<128, 256, 2, 2, 32, 3, true, false, true>>(g, st);
+    if (size == kHiddenMid) return launch_up_as<ACT, Tile<128, 128, 2, 2, 64, 2, true, false, true>>(g, st);
+    return launch_up_as<ACT, Tile<64, 128, 2, 2, 64, 4, true, false, true>>(g, st);
+}
+
+template <int ACT, typename C, typename C2>
+int launch_hidden_as(const HiddenArgs& g, hipStream_t st) {
+    BPT_LAUNCH("gated_hidden_bwd_kernel", (gated_hidden_bwd_kernel<C, C2, ACT>), dim3((unsigned)((int64_t)g.tiles_m * g.tiles_n)),
+               dim3(C::kThreads), 0, st, g);
     BPT_HIP(hipGetLastError());
     return BPT_OK;
 }
-
 template <int ACT>
 int launch_hidden(HiddenArgs& g, hipStream_t st) {
-    const bool wide = wide_hidden(g.M, g.f);
-    g.tiles_m = (int)((g.M + 127) / 128);
-    g.tiles_n = wide ? (g.f + 127) / 128 : (g.f + 63) / 64;
-    const dim3 grid((unsigned)((int64_t)g.tiles_m * g.tiles_n));
-    using Wide = Tile<128, 256, 1, 4, 32, 3, true, false, true>;
-    using Wide2 = Tile<128, 128, 1, 4, 32, 3, true, true, false>;
-    using Mid = Tile<128, 128, 2, 2, 64, 2, true, false, true>;
-    using Mid2 = Tile<128, 64, 2, 2, 64, 2, true, true, false>;
-    if (wide) BPT_LAUNCH("gated_hidden_bwd_kernel", (gated_hidden_bwd_kernel<Wide, Wide2, ACT>), grid, dim3(Wide::kThreads), 0, st, g);
-    else BPT_LAUNCH("gated_hidden_bwd_kernel", (gated_hidden_bwd_kernel<Mid, Mid2, ACT>), grid, dim3(Mid::kThreads), 0, st, g);
-    BPT_HIP(hipGetLastError());
-    return BPT_OK;
+    const HiddenSize size = hidden_tiles(g.M, g.f, true, g.tiles_m, g.tiles_n);
+    if (size == kHiddenBig)
+        return launch_hidden_as<ACT, Tile<256, 256, 2, 4, 64, 2, true, false, true>, Tile<256, 128, 2, 4, 64, 2, true, true, false>>(g, st);
+    if (size == kHiddenWide)
+        return launch_hidden_as<ACT, Tile<128, 256, 1, 4, 32, 3, true, false, true>, Tile<128, 128, 1, 4, 32, 3, true, true, false>>(g, st);
+    if (size == kHiddenMid)
+        return launch_hidden_as<ACT, Tile<128, 128, 2, 2, 64, 2, true, false, true>, Tile<128, 64, 2, 2, 64, 2, true, true, false>>(g, st);
+    return launch_hidden_as<ACT, Tile<64, 128, 2, 2, 64, 4, true, false, true>, Tile<64, 64, 2, 2, 64, 4, true, true, false>>(g, st);
 }
 
 int check_ffn(const bpt_gated_ffn_t* s) {
@@ -413,8 +509,8 @@ int check_ffn(const bpt_gated_ffn_t* s) {
     if (s->stride < s->d || (s->stride & 7) || s->stride >= ((int64_t)1 << 20)) return BPT_ERR_INVALID_ARG;
     if (s->activation < BPT_ACT_SILU || s->activation > BPT_ACT_RELU) return BPT_ERR_INVALID_ARG;
     if (s->grad_dtype != BPT_F32 && s->grad_dtype != BPT_BF16) return BPT_ERR_INVALID_ARG;
-    // tiles are numbered in 31 bits (of 128 x 64 at least)
-    if (((s->rows + 127) / 128) * ((std::max(s->d, s->f) + 63) / 64) > INT32_MAX) return BPT_ERR_UNSUPPORTED;
+    // tiles are numbered in 31 bits (of 64 x 64 at least)
+    if (((s->rows + 63) / 64) * ((std::max(s->d, s->f) + 63) / 64) > INT32_MAX) return BPT_ERR_UNSUPPORTED;
     return BPT_OK;
 }
 
@@ -427,7 +523,7 @@ FwdBuffers fwd_buffers(const bpt_gated_ffn_t* s) {
     b.down = plan_product(s->rows, s->d, s->f, 1, 1);
     b.F = 0;
     b.part = align256((size_t)s->rows * s->f * 2);
-    b.total = b.part + part_bytes(b.down);
+    b.total = b.part + (use_strips(s->rows, s->d) ? 0 : part_bytes(b.down));
     return b;
 }
 struct BwdBuffers {
@@ -495,6 +591,12 @@ int bpt_gated_ffn_fwd(const bpt_gated_ffn_t* s, const void* X, const void* Wg, c
     const int rc = s->activation == BPT_ACT_SILU ? launch_up<BPT_ACT_SILU>(u, st)
                    : s->activation == BPT_ACT_GELU ? launch_up<BPT_ACT_GELU>(u, st) : launch_up<BPT_ACT_RELU>(u, st);
     if (rc) return rc;
+    if (use_strips(s->rows, s->d)) {
+        const DownArgs g = {F, static_cast<const bf16_t*>(Wd), static_cast<bf16_t*>(Y), s->rows, s->stride, s->d, s->f};
+        BPT_LAUNCH("down_strip_kernel", down_strip_kernel, strip_grid(s->rows, s->d), dim3(DownStrip::kThreads), 0, st, g);
+        BPT_HIP(hipGetLastError());
+        return BPT_OK;
+    }
     ProductArgs g = {};
     g.A[0] = g.A[1] = F; g.B[0] = g.B[1] = static_cast<const bf16_t*>(Wd); g.C[0] = g.C[1] = Y;
     g.M = s->rows; g.N = s->d; g.K = s->f;

@@ -19,6 +19,7 @@ namespace bpt {
 namespace {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef int i32x2_t __attribute__((ext_vector_type(2)));
 typedef int i32x4_t __attribute__((ext_vector_type(4)));
@@ -142,6 +143,8 @@ struct Tile {
     using LoadB = SlabLoader<kBWidth, kWaves, B_KFIRST, SLAB>;
     static constexpr int kStage = LoadA::kBytes + LoadB::kBytes * (PAIR ? 2 : 1);
     static constexpr int kLds = STAGES * kStage;
+    static constexpr int kWavesPerSimd = kWaves == 8 || 2 * kLds <= 160 * 1024 ? 2 : 1;
+    static_assert(STAGES >= 2 && STAGES <= 4, "run() has waits for these");
     static constexpr int kPending = (LoadA::kLoads + LoadB::kLoads * (PAIR ? 2 : 1));   // loads of a slab, per wavefront
     typedef f32x16_t Acc[kRows][kCols];
 
@@ -207,8 +210,10 @@ struct Tile {
             }
         int stage = 0, next = STAGES - 1;
         for (int t = 0; t < slabs; ++t) {
-            if (STAGES == 2 || t + 1 == slabs) slab_barrier<0>();
-            else slab_barrier<kPending * (STAGES - 2)>();
+            const int behind = min(STAGES - 2, slabs - 1 - t);   // slabs that may still be on their way
+            if (STAGES > 3 && behind == 2) slab_barrier<(STAGES > 3 ? 2 : 0) * kPending>();
+            else if (STAGES > 2 && behind == 1) slab_barrier<(STAGES > 2 ? 1 : 0) * kPending>();
+            else slab_barrier<0>();
             if (t + STAGES - 1 < slabs) {
                 from(t + STAGES - 1, a, b0, b1, k_left);
                 load(a, b0, b1, k_left, next);
@@ -220,6 +225,78 @@ struct Tile {
         slab_barrier<0>();
     }
 };
+// For few rows: 32 x 32 of C (PAIR: of two products with the same A) in a workgroup, whose WAVES wavefronts each take a
+// part of k with slabs, loads and waits of their own, so that all of them keep loads of the weights in flight; their sums
+// meet in LDS at the end.  A and B as in a Tile with k contiguous in A and n in B.
+template <int WAVES, int STAGES, bool PAIR>
+struct Strip {
+    static constexpr int kSlab = 32, kThreads = 64 * WAVES, kMats = PAIR ? 2 : 1;
+    using LoadA = SlabLoader<32, 1, true, kSlab>;
+    using LoadB = SlabLoader<32, 1, false, kSlab>;
+    static constexpr int kStage = LoadA::kBytes + kMats * LoadB::kBytes;
+    static constexpr int kPending = LoadA::kLoads + kMats * LoadB::kLoads;
+    static constexpr int kLds = WAVES * STAGES * kStage;
+    static_assert(STAGES == 4 && WAVES >= 4 && kLds >= WAVES * kMats * 4096, "waits and the final sums are written for these");
+    typedef f32x16_t Acc[kMats];
+
+    // On return wavefront w < 4 holds in sum[mat] C[lane % 32][8 w + 4 (lane / 32) ..+ 3].  a: first row's k = 0; b: first column's.
+    static __device__ __forceinline__ void run(unsigned char* shared, int wave, int lane, const bf16_t* a, int64_t lda, int64_t rows,
+                                               const bf16_t* const* b, int64_t ldb, int cols, int64_t k_from, int64_t k_to, float4* sum) {
+        lds_bytes_t all = (lds_bytes_t)shared, mine = all + wave * STAGES * kStage;
+        LoadA la;
+        LoadB lb;
+        la.init(0, lane, lda, rows);
+        lb.init(0, lane, ldb, cols);
+        const int slabs = (int)((k_to - k_from + kSlab - 1) / kSlab), each = (slabs + WAVES - 1) / WAVES;
+        const int count = max(min(each, slabs - wave * each), 0);
+        const int64_t k0 = k_from + (int64_t)wave * each * kSlab;
+        auto load = [&](int t) {
+            const int64_t k = k0 + (int64_t)t * kSlab;
+            lds_bytes_t p = mine + (t & (STAGES - 1)) * kStage;
+            la.load(a + k, k_to - k, p, 0, lane);
+#pragma unroll
+            for (int m = 0; m < kMats; ++m) lb.load(b[m] + k * ldb, k_to - k, p + LoadA::kBytes + m * LoadB::kBytes, 0, lane);
+        };
+        Acc acc = {};
+        for (int t = 0; t < min(STAGES - 1, count); ++t) load(t);
+        for (int t = 0; t < count; ++t) {
+            // this slab has arrived (those behind it may be on their way), and the reads of the one before are through
+            const int behind = count - 1 - t;
+            if (behind >= 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(2 * kPending) : "memory");
+            else if (behind == 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(kPending) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            if (t + STAGES - 1 < count) load(t + STAGES - 1);
+            lds_bytes_t p = mine + (t & (STAGES - 1)) * kStage;
+#pragma unroll
+            for (int kk = 0; kk < kSlab / 16; ++kk) {
+                const bf16x8_t x = fragment<32, true, kSlab>(p, 0, kk, lane);
+#pragma unroll
+                for (int m = 0; m < kMats; ++m)
+                    acc[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fragment<32, false, kSlab>(p + LoadA::kBytes + m * LoadB::kBytes, 0, kk, lane), x,
+                                                                     acc[m], 0, 0, 0);
+            }
+        }
+        slab_barrier<0>();   // (the sums take the slabs' place)
+        typedef __attribute__((address_space(3))) f32x4_t* ptr_t;
+#pragma unroll
+        for (int m = 0; m < kMats; ++m)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const f32x4_t v = {acc[m][4 * q], acc[m][4 * q + 1], acc[m][4 * q + 2], acc[m][4 * q + 3]};
+                *(ptr_t)(all + ((wave * kMats + m) * 4 + q) * 1024 + lane * 16) = v;
+            }
+        __syncthreads();
+        if (wave < 4)
+#pragma unroll
+            for (int m = 0; m < kMats; ++m) {
+                f32x4_t v = {};
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) v += *(ptr_t)(all + ((w * kMats + m) * 4 + wave) * 1024 + lane * 16);
+                sum[m] = make_float4(v[0], v[1], v[2], v[3]);
+            }
+    }
+};
+
 // Rounds 32 rows of a wavefront's COLS columns to bf16 and writes them, through LDS of its own, in 16-byte pieces along the
 // rows (from the accumulators' order a store would touch 32 rows for 16 bytes each).  A wavefront's LDS accesses are in
 // order, so nothing is waited for between blocks of rows.
@@ -240,10 +317,12 @@ struct RowBlock {
         typedef __attribute__((address_space(3))) const i32x4_t* ptr_t;
         constexpr int kPieces = COLS / 8, kRows = 64 / kPieces;
         const int r = lane / kPieces, c = lane % kPieces * 8;
+        const uint32_t at = (uint32_t)(r * (int)ld + c) * 2;   // (the rest of the address is the wavefront's)
+        const int last = c < cols ? (int)min((int64_t)32, rows) - r : 0;
 #pragma unroll
         for (int i = 0; i < 32; i += kRows) {
             const i32x4_t v = *(ptr_t)(lds + (i + r) * kPitch + c * 2);
-            if (i + r < rows && c < cols) *reinterpret_cast<i32x4_t*>(out + (i + r) * ld + c) = v;
+            if (i < last) *reinterpret_cast<i32x4_t*>(reinterpret_cast<unsigned char*>(out + i * ld) + at) = v;
         }
     }
 };
