@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(RowTeam<THREADS>::kBlock) residual_norm_kernel
 // fp32 as the forward did, not from its rounded copy), six values of memory traffic per element; the sums stay in the
 // thread's registers over all rows of its workgroup.
 template <typename T, int THREADS>
-__global__ void __launch_bounds__(RowTeam<THREADS>::kBlock) residual_norm_bwd_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(RowTeam<THREADS>::kBlock, 2) residual_norm_bwd_kernel(const NormArgs a) {
     using Team = RowTeam<THREADS>;
     __shared__ float2 lds[2 * Team::kBlock / 64];
     __shared__ float gather[Team::kRows > 1 ? (Team::kRows - 1) * THREADS * 8 : 1];
@@ -193,32 +193,36 @@ __global__ void __launch_bounds__(RowTeam<THREADS>::kBlock) residual_norm_bwd_ke
         const int64_t group = unit / a.slices, slice = unit - group * a.slices;
         const int64_t begin = group * a.group_rows + slice * a.unit_rows;
         const int64_t end = min(min(begin + a.unit_rows, (group + 1) * a.group_rows), a.rows);
-        int64_t row = begin + team;
-        Raw8<T> xw = {}, bw = {}, gw = {}, dyw = {}, dhw = {};
-        float4 st = make_float4(0.f, 1.f, 0.f, 1.f);
-        if (pg && !gate_each && has && begin < end) gw.load(pg + group * a.d + col);
-        auto fetch = [&](int64_t r) {
+        // as many rows are on their way as registers allow: two in bf16, one in fp32
+        constexpr int kAhead = sizeof(T) == 2 ? 2 : 1;
+        struct Row {
+            Raw8<T> x, b, g, dy, dh;
+            float4 st;
+        } rows[kAhead] = {};
+        Raw8<T> gate = {};
+        if (pg && !gate_each && has && begin < end) gate.load(pg + group * a.d + col);
+        auto fetch = [&](Row& w, int64_t r) {
+            w.st = make_float4(0.f, 1.f, 0.f, 1.f);
             if (r >= end) return;
-            st = a.stats[r];
+            w.st = a.stats[r];
             if (!has) return;
             const int64_t at = r * a.stride + col;
-            xw.load(px + at);
-            if (pb) bw.load(pb + at);
-            if (pdy) dyw.load(pdy + at);
-            if (pdh) dhw.load(pdh + at);
-            if (gate_each) gw.load(pg + r * a.d + col);
+            w.x.load(px + at);
+            if (pb) w.b.load(pb + at);
+            if (pdy) w.dy.load(pdy + at);
+            if (pdh) w.dh.load(pdh + at);
+            if (gate_each) w.g.load(pg + r * a.d + col);
         };
-        fetch(row);
-        for (int64_t at = begin; at < end; at += Team::kRows, row += Team::kRows) {
+        auto work = [&](Row& w, int64_t row) {
             const bool live = has && row < end;
             float x[8], b[8], g[8], dy[8], dh[8];
-            xw.get(x);
-            bw.get(b);
-            gw.get(g);
-            dyw.get(dy);
-            dhw.get(dh);
-            const float4 s = st;
-            fetch(row + Team::kRows);
+            w.x.get(x);
+            w.b.get(b);
+            (gate_each ? w.g : gate).get(g);
+            w.dy.get(dy);
+            w.dh.get(dh);
+            const float4 s = w.st;
+            fetch(w, row + kAhead * Team::kRows);
             float bn[8];   // post(branch)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -287,6 +291,12 @@ __global__ void __launch_bounds__(RowTeam<THREADS>::kBlock) residual_norm_bwd_ke
                 for (int e = 0; e < 8; ++e) dy[e] = s.y * (dy[e] * g1[e] - m1 - b[e] * m2);
             }
             if (live && a.d_branch) store8(static_cast<T*>(a.d_branch) + row * a.stride + col, dy);
+        };
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) fetch(rows[i], begin + team + i * Team::kRows);
+        for (int64_t at = begin; at < end; at += kAhead * Team::kRows) {
+            work(rows[0], at + team);
+            if (kAhead == 2 && at + Team::kRows < end) work(rows[kAhead - 1], at + team + Team::kRows);
         }
         if (pg && !gate_each) {
             over_teams(sum_gate);
@@ -298,6 +308,7 @@ __global__ void __launch_bounds__(RowTeam<THREADS>::kBlock) residual_norm_bwd_ke
             for (int e = 0; e < 8; ++e) sum_gate[e] = 0.f;
         }
     }
+#pragma unroll
     for (int i = 0; i < 4; ++i)
         if (a.sum_at[i] >= 0) {
             over_teams(sums[i]);
@@ -353,7 +364,8 @@ __global__ void __launch_bounds__(256) norm_column_sum_kernel(const SumJobs a) {
     }
 }
 
-constexpr int kNormBlocks = 5 * 256, kNormBwdBlocks = 2 * 256;   // workgroups (of 256 threads) that walk over the rows
+// compute units; workgroups of 256 threads that are resident on one: forward 5 (bf16) and 4 (fp32), backward 2
+constexpr int kNormBlocks = 256, kNormBwdBlocks = 2 * 256;
 
 int norm_threads(int d) {
     int t = 16;
@@ -402,8 +414,10 @@ BwdPlan bwd_plan(const bpt_residual_norm_t* s) {
 template <typename T, int THREADS>
 int launch_fwd(const NormArgs& a, hipStream_t st) {
     using Team = RowTeam<THREADS>;
-    const int64_t most = std::max(1, kNormBlocks * 256 / Team::kBlock);
-    const dim3 grid((unsigned)std::min<int64_t>(most, (a.rows + Team::kRows - 1) / Team::kRows));
+    // as many workgroups as are resident, of equal shares of the rows
+    const int64_t most = (int64_t)kNormBlocks * (sizeof(T) == 2 ? 5 : 4) * 256 / Team::kBlock;
+    const int64_t groups = (a.rows + Team::kRows - 1) / Team::kRows, each = (groups + most - 1) / most;
+    const dim3 grid((unsigned)((groups + each - 1) / each));
     BPT_LAUNCH("residual_norm_kernel", (residual_norm_kernel<T, THREADS>), grid, dim3(Team::kBlock), 0, st, a);
     BPT_HIP(hipGetLastError());
     return BPT_OK;

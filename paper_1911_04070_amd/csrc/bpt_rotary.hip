@@ -16,115 +16,145 @@ struct RotaryArgs {
     const float* pos;
     int64_t pos_sb;
     int64_t sb, sh, sn, ob, oh, on;   // elements
-    int64_t items;                    // B * N * items per row
-    int32_t N, H, heads_each, rot;
+    int64_t rows;                     // B * N
+    int32_t N, H, rot;
+    int32_t each;                     // rows of a workgroup, a power of two
+    int32_t heads_first;              // the heads of a row lie closer together than its neighbours
     double turns[kD / 2];             // w_i' / (2 pi), negative for the inverse
 };
 
-// V consecutive values of a row
-template <typename T, int V>
-struct alignas(sizeof(T) * V) Pack {
-    T x[V];
+// 16 bytes of a row
+template <typename T>
+struct Piece {
+    static constexpr int kCount = 16 / sizeof(T);
+    T x[kCount];
+    __device__ __forceinline__ void load(const T* p) {
+        const uint4 w = *reinterpret_cast<const uint4*>(p);
+        __builtin_memcpy(x, &w, 16);
+    }
+    __device__ __forceinline__ void store(T* p) const {
+        uint4 w;
+        __builtin_memcpy(&w, x, 16);
+        *reinterpret_cast<uint4*>(p) = w;
+    }
 };
 __device__ __forceinline__ float to_f32(bf16_t x) { return bf16_as_f32(x); }
 __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ void from_f32(float v, bf16_t& x) { x = __builtin_bit_cast(uint16_t, (__bf16)v); }
 __device__ __forceinline__ void from_f32(float v, float& x) { x = v; }
 
-// A thread owns one item of a row -- V pairs, 2 V features -- and turns it in `heads_each` heads of Q and K, so that
-// an angle's sine and cosine (64-bit product, reduced to a turn, then fp32) are formed once for up to 2 H uses.
-// HALVES: the pairs' first features are V consecutive ones, the second ones V more, rot / 2 further on; else a pair
-// is two neighbours.  Items behind rot / (2 V) are features that are copied.  V is the largest of 8 (fp32: 4), 4, 2, 1
-// that divides rot / 2, so that an access is 16 bytes wherever the layout allows it.
-template <typename T, int V, bool HALVES, int NT>
+enum PairLayout { kNeighbours, kHalves, kHalvesApart };   // kHalvesApart: a half is not a whole number of 16-byte pieces
+
+// A workgroup forms the sines and cosines of its `each` rows once, one or a few per thread, into LDS (64-bit product, reduced to a
+// turn, then fp32), and turns all heads of Q and K with them.  A thread takes 16 bytes of a row; 8 (fp32: 16) lanes cover a
+// head's row, the next lanes the next head or the next row, whichever lies behind it, so that loads and stores are whole cache
+// lines.  With halves a thread also loads the 16 bytes its features are paired with, which its neighbours have just asked
+// for, and computes its own side of the pairs only.  (Lanes that hold both halves of a pair, in 64 bytes of two lines each:
+// 16 383 rows x 4 x 8 heads, bf16: 78 us.)  Bound by HBM.
+// A result may overwrite its input: a pair's threads are lanes of one wavefront, which loads before it stores.
+constexpr int kRotaryRows = 16;
+template <typename T, PairLayout LAYOUT, int NT>
 __global__ void __launch_bounds__(256) rotary_kernel(const RotaryArgs a) {
-    constexpr int kItems = kD / (2 * V);
-    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (t >= a.items) return;
-    const int item = (int)(t % kItems);
-    const uint32_t row = (uint32_t)(t / kItems);
-    const uint32_t b = row / (uint32_t)a.N, n = row - b * (uint32_t)a.N;
-    const int h0 = blockIdx.y * a.heads_each, h1 = min(a.H, h0 + a.heads_each);
-    const bool turned = item * 2 * V < a.rot;
-    const int at0 = turned && HALVES ? item * V : item * 2 * V;
-    const int at1 = turned && HALVES ? a.rot / 2 + item * V : item * 2 * V + V;
-    float c[V], s[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        c[v] = 1.f;
-        s[v] = 0.f;
-    }
-    if (turned) {
-        const double p = (double)a.pos[(int64_t)b * a.pos_sb + n];
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const double x = p * a.turns[item * V + v];
-            sincospif(2.f * (float)(x - rint(x)), &s[v], &c[v]);
+    constexpr int kPieces = kD / Piece<T>::kCount, kCount = Piece<T>::kCount, kSlots = 256 / kPieces;
+    __shared__ float2 table[kRotaryRows][kD / 2 + 2];   // (two more: rows start in different banks)
+    __shared__ int64_t in_row[kRotaryRows], out_row[kRotaryRows];
+    const int64_t first = (int64_t)blockIdx.x * a.each;
+    const int rows = (int)min((int64_t)a.each, a.rows - first);
+    for (int t = threadIdx.x; t < rows * (kD / 2); t += 256) {
+        const int r = t / (kD / 2), i = t % (kD / 2);
+        const uint32_t row = (uint32_t)(first + r), b = row / (uint32_t)a.N, n = row - b * (uint32_t)a.N;
+        if (i == 0) {
+            in_row[r] = (int64_t)b * a.sb + (int64_t)n * a.sn;
+            out_row[r] = (int64_t)b * a.ob + (int64_t)n * a.on;
         }
+        float2 v = make_float2(1.f, 0.f);
+        if (i < a.rot / 2) {
+            const double x = (double)a.pos[(int64_t)b * a.pos_sb + n] * a.turns[i];
+            sincospif(2.f * (float)(x - rint(x)), &v.y, &v.x);
+        }
+        table[r][i] = v;
     }
-    const int64_t in_at = (int64_t)b * a.sb + (int64_t)n * a.sn, out_at = (int64_t)b * a.ob + (int64_t)n * a.on;
+    __syncthreads();
+    // slot = (row, head), heads or rows running fastest; a thread steps kSlots slots at a time
+    const int f0 = (int)(threadIdx.x % kPieces) * kCount, slots = rows * a.H, half = a.rot / 2;
+    int slot = threadIdx.x / kPieces;
+    const int inner = a.heads_first ? a.H : rows;
+    int lo = slot % inner, hi = slot / inner;
+    const int lo_step = kSlots % inner, hi_step = kSlots / inner;
+    const bool second = f0 >= half;
 #pragma unroll 2
-    for (int h = h0; h < h1; ++h) {
-        Pack<T, V> x0[NT], x1[NT];
+    for (; slot < slots; slot += kSlots) {
+        const int h = a.heads_first ? lo : hi, r = a.heads_first ? hi : lo;
+        const int64_t in_at = in_row[r] + h * a.sh + f0, out_at = out_row[r] + h * a.oh + f0;
+        Piece<T> x[NT], y[NT];
 #pragma unroll
         for (int w = 0; w < NT; ++w) {
-            const T* p = static_cast<const T*>(a.in[w]) + in_at + h * a.sh;
-            x0[w] = *reinterpret_cast<const Pack<T, V>*>(p + at0);
-            x1[w] = *reinterpret_cast<const Pack<T, V>*>(p + at1);
+            const T* p = static_cast<const T*>(a.in[w]) + in_at;
+            x[w].load(p);
+            if (LAYOUT == kHalves && f0 < a.rot) y[w].load(second ? p - half : p + half);
+            if (LAYOUT == kHalvesApart)
+#pragma unroll
+                for (int e = 0; e < kCount; ++e) {
+                    const int f = f0 + e;
+                    if (f < a.rot) y[w].x[e] = f < half ? p[e + half] : p[e - half];
+                }
         }
 #pragma unroll
         for (int w = 0; w < NT; ++w) {
-            T* p = static_cast<T*>(a.out[w]) + out_at + h * a.oh;
-            if (turned) {
-                T x[2 * V];
+            Piece<T> o = x[w];
+            if (LAYOUT == kNeighbours) {
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    x[v] = x0[w].x[v];
-                    x[V + v] = x1[w].x[v];
-                }
+                for (int e = 0; e < kCount; e += 2)
+                    if (f0 + e < a.rot) {
+                        const float2 t = table[r][(f0 + e) / 2];
+                        const float u = to_f32(x[w].x[e]), v = to_f32(x[w].x[e + 1]);
+                        from_f32(u * t.x - v * t.y, o.x[e]);
+                        from_f32(v * t.x + u * t.y, o.x[e + 1]);
+                    }
+            } else {
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const int i = HALVES ? v : 2 * v, j = HALVES ? V + v : 2 * v + 1;
-                    const float f = to_f32(x[i]), g = to_f32(x[j]);
-                    from_f32(f * c[v] - g * s[v], x[i]);
-                    from_f32(g * c[v] + f * s[v], x[j]);
-                }
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    x0[w].x[v] = x[v];
-                    x1[w].x[v] = x[V + v];
+                for (int e = 0; e < kCount; ++e) {
+                    const int f = f0 + e;
+                    const bool is_second = LAYOUT == kHalves ? second : f >= half;
+                    if (LAYOUT == kHalves ? f0 < a.rot : f < a.rot) {
+                        const float2 t = table[r][is_second ? f - half : f];
+                        from_f32(to_f32(x[w].x[e]) * t.x + to_f32(y[w].x[e]) * (is_second ? t.y : -t.y), o.x[e]);
+                    }
                 }
             }
-            *reinterpret_cast<Pack<T, V>*>(p + at0) = x0[w];
-            *reinterpret_cast<Pack<T, V>*>(p + at1) = x1[w];
+            o.store(static_cast<T*>(a.out[w]) + out_at);
+        }
+        lo += lo_step;
+        hi += hi_step;
+        if (lo >= inner) {
+            lo -= inner;
+            ++hi;
         }
     }
 }
 
-// heads per thread: all of them where the rows alone fill the device, fewer for few rows (a decoding step is one row
-// of every sequence), down to one
-int heads_each(int64_t items, int H) {
-    const int64_t threads = (int64_t)256 * 2048;   // what 256 compute units hold
-    const int64_t parts = std::min<int64_t>(H, std::max<int64_t>(1, threads / std::max<int64_t>(items, 1)));
-    return (int)((H + parts - 1) / parts);
+// rows of a workgroup: 16, fewer where that leaves compute units idle (a decoding step is one row of every sequence)
+int rotary_rows(int64_t rows) {
+    int each = kRotaryRows;
+    while (each > 1 && rows / each < 1024) each /= 2;
+    return each;
 }
 
-template <typename T, int V, bool HALVES>
-int launch_rotary(RotaryArgs& a, int64_t rows, hipStream_t st) {
-    constexpr int kItems = kD / (2 * V);
-    a.items = rows * kItems;
-    a.heads_each = heads_each(a.items, a.H);
-    const dim3 grid((unsigned)((a.items + 255) / 256), (unsigned)((a.H + a.heads_each - 1) / a.heads_each));
+template <typename T, PairLayout LAYOUT>
+int launch_rotary(RotaryArgs& a, hipStream_t st) {
+    a.each = rotary_rows(a.rows);
+    const dim3 grid((unsigned)((a.rows + a.each - 1) / a.each));
     if (a.in[1])
-        BPT_LAUNCH("rotary_kernel", (rotary_kernel<T, V, HALVES, 2>), grid, dim3(256), 0, st, a);
+        BPT_LAUNCH("rotary_kernel", (rotary_kernel<T, LAYOUT, 2>), grid, dim3(256), 0, st, a);
     else
-        BPT_LAUNCH("rotary_kernel", (rotary_kernel<T, V, HALVES, 1>), grid, dim3(256), 0, st, a);
+        BPT_LAUNCH("rotary_kernel", (rotary_kernel<T, LAYOUT, 1>), grid, dim3(256), 0, st, a);
     BPT_HIP(hipGetLastError());
     return BPT_OK;
 }
-template <typename T, int V>
-int launch_rotary(RotaryArgs& a, int64_t rows, bool interleaved, hipStream_t st) {
-    return interleaved ? launch_rotary<T, V, false>(a, rows, st) : launch_rotary<T, V, true>(a, rows, st);
+template <typename T>
+int launch_rotary(RotaryArgs& a, bool interleaved, hipStream_t st) {
+    if (interleaved) return launch_rotary<T, kNeighbours>(a, st);
+    return (a.rot / 2) % Piece<T>::kCount ? launch_rotary<T, kHalvesApart>(a, st) : launch_rotary<T, kHalves>(a, st);
 }
 
 // no two rows of [B][H][N][kD] with these strides overlap: see bpt_rotary_t
@@ -203,6 +233,8 @@ int bpt_rotary(const bpt_rotary_t* s, const float* pos, int64_t pos_stride_b, co
     a.sb = in[0]; a.sh = in[1]; a.sn = in[2];
     a.ob = out[0]; a.oh = out[1]; a.on = out[2];
     a.N = s->N; a.H = s->H; a.rot = s->rot;
+    a.rows = rows;
+    a.heads_first = in[1] < in[2];
     const double kTwoPi = 6.283185307179586476925286766559;
     const double step = std::pow(base, -2.0 / s->rot);
     double w = 1.0;   // 32 products of the step at most: relative error below 32 * 2^-53
@@ -212,17 +244,7 @@ int bpt_rotary(const bpt_rotary_t* s, const float* pos, int64_t pos_stride_b, co
         a.turns[i] = w * (keep + (1.0 - keep) / factor) / kTwoPi * (s->inverse ? -1.0 : 1.0);
     }
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const bool il = s->interleaved != 0;
-    const int half = s->rot / 2;
-    if (s->dtype == BPT_BF16) {
-        if (half % 8 == 0) return launch_rotary<bf16_t, 8>(a, rows, il, st);
-        if (half % 4 == 0) return launch_rotary<bf16_t, 4>(a, rows, il, st);
-        if (half % 2 == 0) return launch_rotary<bf16_t, 2>(a, rows, il, st);
-        return launch_rotary<bf16_t, 1>(a, rows, il, st);
-    }
-    if (half % 4 == 0) return launch_rotary<float, 4>(a, rows, il, st);
-    if (half % 2 == 0) return launch_rotary<float, 2>(a, rows, il, st);
-    return launch_rotary<float, 1>(a, rows, il, st);
+    return s->dtype == BPT_BF16 ? launch_rotary<bf16_t>(a, s->interleaved != 0, st) : launch_rotary<float>(a, s->interleaved != 0, st);
 }
 
 int bpt_node_positions(const bpt_graph_t* g, float* pos, void* stream) {
