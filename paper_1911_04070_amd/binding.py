@@ -726,6 +726,8 @@ def _on_device(x: torch.Tensor, what: str) -> torch.device:
 
 def _rotary_out(x: torch.Tensor) -> torch.Tensor:
     """A dense [B,H,N,D] tensor with x's order of heads and rows."""
+    if x.is_contiguous():
+        return torch.empty_like(x)      # (half the host time of torch.empty, which a decoding step notices)
     B, H, N, D = x.shape
     if H > 1 and N > 1 and x.stride(1) < x.stride(2):
         return torch.empty((B, N, H, D), dtype=x.dtype, device=x.device).permute(0, 2, 1, 3)
@@ -789,6 +791,10 @@ def _row_stride(x: torch.Tensor, what: str) -> int:
     return stride
 
 
+def _same_strides(x: torch.Tensor) -> torch.Tensor:
+    return torch.empty_like(x) if x.is_contiguous() else torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device)
+
+
 def _like(x: torch.Tensor, t: torch.Tensor, what: str) -> None:
     if t.dtype != x.dtype or t.shape != x.shape or t.stride() != x.stride() or t.device != x.device:
         raise ValueError("%s must have the dtype, shape, strides and device of x" % what)
@@ -824,8 +830,8 @@ def bpt_residual_norm_fwd(x: torch.Tensor, branch: Optional[torch.Tensor], gate:
     x, branch: [..., d] in fp32 or bf16, equal layouts; gate: [ceil(rows / gate_rows), d] in their type, each row for gate_rows
     consecutive rows; gains and biases fp32 [d] or None.  Returns (y, h), with want_stats (y, h, stats) for the backward."""
     s = _norm_args(x, branch, gate, post, pre, post_gain, post_bias, pre_gain, pre_bias, gate_rows, residual_scale, eps)
-    y = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device)
-    h = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device) if s.pre else None
+    y = _same_strides(x)
+    h = _same_strides(x) if s.pre else None
     stats = torch.empty((s.rows, 4), dtype=torch.float32, device=x.device) if want_stats else None
     _check(load_library().bpt_residual_norm_fwd(ctypes.byref(s), x.data_ptr(), _ptr(branch), _ptr(gate), _ptr(post_gain), _ptr(post_bias),
                                                 _ptr(pre_gain), _ptr(pre_bias), y.data_ptr(), _ptr(h), _ptr(stats), _raw_stream(x.device.index)),
@@ -849,9 +855,9 @@ def bpt_residual_norm_bwd(x: torch.Tensor, branch: Optional[torch.Tensor], gate:
     if stats.dtype != torch.float32 or tuple(stats.shape) != (s.rows, 4) or not stats.is_contiguous() or stats.device != x.device:
         raise ValueError("stats must be what the forward returned")
     L = load_library()
-    out = {"dx": torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device)}
+    out = {"dx": _same_strides(x)}
     if branch is not None:
-        out["d_branch"] = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device)
+        out["d_branch"] = _same_strides(x)
     for name, p in (("d_gate", gate), ("d_post_gain", post_gain), ("d_post_bias", post_bias), ("d_pre_gain", pre_gain),
                     ("d_pre_bias", pre_bias)):
         if p is not None:
@@ -887,7 +893,7 @@ def bpt_gated_ffn_fwd(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: t
     s = _ffn_args(X, Wg, Wu, Wd, activation)
     L = load_library()
     if out is None:
-        out = torch.empty_strided(X.shape, X.stride(), dtype=X.dtype, device=X.device)
+        out = _same_strides(X)
     else:
         _like(X, out, "out")
     need = _need(int(L.bpt_gated_ffn_fwd_workspace(ctypes.byref(s))), "bpt_gated_ffn_fwd_workspace")
@@ -905,7 +911,7 @@ def bpt_gated_ffn_bwd(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: t
     s = _ffn_args(X, Wg, Wu, Wd, activation, bf16_grads)
     _like(X, dY, "dY")
     L = load_library()
-    dX = torch.empty_strided(X.shape, X.stride(), dtype=X.dtype, device=X.device)
+    dX = _same_strides(X)
     dWg, dWu, dWd = (torch.empty(W.shape, dtype=torch.bfloat16 if bf16_grads else torch.float32, device=X.device) for W in (Wg, Wu, Wd))
     need = _need(int(L.bpt_gated_ffn_bwd_workspace(ctypes.byref(s))), "bpt_gated_ffn_bwd_workspace")
     if workspace is None:

@@ -182,11 +182,10 @@ __device__ __forceinline__ ProductTile product_tile(const ProductArgs& g, int id
     return {mat, (tn - mat * g.tiles_n) * C::kBN, (int64_t)tm * C::kBM};
 }
 template <typename C, bool A_KFIRST, bool B_KFIRST, typename T>
-__global__ void __launch_bounds__(C::kThreads, C::kWavesPerSimd) product_kernel(const ProductArgs g) {
-    __shared__ __attribute__((aligned(1024))) unsigned char shared[C::kLds];
-    const int over = max((int)blockIdx.x - g.full, 0), slice = (int)blockIdx.x < g.full ? 0 : over % g.slices;
-    const bool whole = (int)blockIdx.x < g.full || g.slices == 1;
-    const ProductTile at = product_tile<C>(g, min((int)blockIdx.x, g.full) + over / g.slices);
+__device__ __forceinline__ void product_body(const ProductArgs& g, int group, unsigned char* shared) {
+    const int over = max(group - g.full, 0), slice = group < g.full ? 0 : over % g.slices;
+    const bool whole = group < g.full || g.slices == 1;
+    const ProductTile at = product_tile<C>(g, min(group, g.full) + over / g.slices);
     C t;
     t.init(shared, g.lda, g.M - at.m0, g.ldb, g.N - at.n0);
     typename C::Acc acc = {};
@@ -240,6 +239,25 @@ __global__ void __launch_bounds__(C::kThreads, C::kWavesPerSimd) product_kernel(
                 }
         }
     }
+}
+
+template <typename C, bool A_KFIRST, bool B_KFIRST, typename T>
+__global__ void __launch_bounds__(C::kThreads, C::kWavesPerSimd) product_kernel(const ProductArgs g) {
+    __shared__ __attribute__((aligned(1024))) unsigned char shared[C::kLds];
+    product_body<C, A_KFIRST, B_KFIRST, T>(g, blockIdx.x, shared);
+}
+
+// The three products of the backward at once, dX (the longest sums) first: for few rows none of them fills the device.
+struct GradArgs {
+    ProductArgs dx, wgu, wd;   // whole tiles only
+};
+template <typename CX, typename CW, typename T>
+__global__ void __launch_bounds__(CX::kThreads, CX::kWavesPerSimd) grads_kernel(const GradArgs g) {
+    static_assert(CX::kThreads == CW::kThreads && CX::kLds == CW::kLds, "one launch");
+    __shared__ __attribute__((aligned(1024))) unsigned char shared[CX::kLds];
+    const int group = blockIdx.x, wgu = group - g.dx.full, wd = wgu - g.wgu.full;
+    if (wgu < 0) return product_body<CX, true, true, bf16_t>(g.dx, group, shared);
+    product_body<CW, false, false, T>(wd < 0 ? g.wgu : g.wd, wd < 0 ? wgu : wd, shared);
 }
 
 // The left-over tiles: sums of their slices in order; a workgroup takes one 32 x 32 block of each wavefront.
@@ -544,22 +562,66 @@ BwdBuffers bwd_buffers(const bpt_gated_ffn_t* s) {
     return b;
 }
 
-template <typename T>
-int weight_grads(const bpt_gated_ffn_t* s, const BwdBuffers& b, const bf16_t* X, const bf16_t* dY, unsigned char* ws, void* dWg, void* dWu,
-                 void* dWd, hipStream_t st) {
-    const bf16_t *F = reinterpret_cast<const bf16_t*>(ws + b.F), *dG = reinterpret_cast<const bf16_t*>(ws + b.dG),
-                 *dU = reinterpret_cast<const bf16_t*>(ws + b.dU);
+ProductArgs wd_product(const bpt_gated_ffn_t* s, const bf16_t* F, const bf16_t* dY, void* dWd) {
     ProductArgs g = {};
     g.A[0] = g.A[1] = F; g.B[0] = g.B[1] = dY; g.C[0] = g.C[1] = dWd;
     g.M = s->f; g.N = s->d; g.K = s->rows;
     g.lda = s->f; g.ldb = s->stride; g.ldc = s->d;
     g.terms = g.matrices = 1;
-    if (const int rc = launch_product<false, false, T>(g, b.wd, ws + b.part, st)) return rc;
+    return g;
+}
+ProductArgs wgu_product(const bpt_gated_ffn_t* s, const bf16_t* X, const bf16_t* dG, const bf16_t* dU, void* dWg, void* dWu) {
+    ProductArgs g = {};
     g.A[0] = g.A[1] = X; g.B[0] = dG; g.B[1] = dU; g.C[0] = dWg; g.C[1] = dWu;
-    g.M = s->d; g.N = s->f;
+    g.M = s->d; g.N = s->f; g.K = s->rows;
     g.lda = s->stride; g.ldb = s->f; g.ldc = s->f;
-    g.matrices = 2;
-    return launch_product<false, false, T>(g, b.wgu, ws + b.part, st);
+    g.terms = 1; g.matrices = 2;
+    return g;
+}
+ProductArgs dx_product(const bpt_gated_ffn_t* s, const bf16_t* dG, const bf16_t* dU, const bf16_t* Wg, const bf16_t* Wu, void* dX) {
+    ProductArgs g = {};
+    g.A[0] = dG; g.A[1] = dU; g.B[0] = Wg; g.B[1] = Wu; g.C[0] = g.C[1] = dX;
+    g.M = s->rows; g.N = s->d; g.K = s->f;
+    g.lda = g.ldb = s->f; g.ldc = s->stride;
+    g.terms = 2; g.matrices = 1;
+    return g;
+}
+
+// whole tiles of 64 x 64 of all three products in one launch, where that is estimated shorter than the three one by one
+bool plan_together(const BwdBuffers& b, GradArgs& g) {
+    const TileCost& t = kTileCost[kSmall];
+    int64_t groups = 0, longest = 0, work = 0;
+    for (ProductArgs* p : {&g.dx, &g.wgu, &g.wd}) {
+        const int64_t slabs = (p->K + t.slab - 1) / t.slab * p->terms, tm = (p->M + t.m - 1) / t.m, tn = (p->N + t.n - 1) / t.n;
+        if (tm * tn * p->matrices > 1 << 20) return false;
+        p->tiles_m = (int)tm;
+        p->tiles_n = (int)tn;
+        p->full = (int)(tm * tn * p->matrices);
+        p->slices = 1;
+        p->slice_slabs = (int)slabs;
+        groups += p->full;
+        longest = std::max(longest, slabs);
+        work += p->full * slabs;
+    }
+    const float us = groups <= kCus ? t.us_alone : t.us;
+    const float together = kStartUs + us * std::max((float)longest, (float)work / (kCus * t.per_cu));
+    return together < b.dx.us + b.wgu.us + b.wd.us;
+}
+
+template <typename T>
+int grads(const bpt_gated_ffn_t* s, const BwdBuffers& b, GradArgs& g, bool dx_alone, void* part, hipStream_t st) {
+    if (s->rows > 0 && !dx_alone && plan_together(b, g)) {
+        using CX = Tile<64, 64, 2, 2, 64, 4, true, true, false>;
+        using CW = Tile<64, 64, 2, 2, 64, 4, false, false, false>;
+        BPT_LAUNCH("grads_kernel", (grads_kernel<CX, CW, T>), dim3((unsigned)(g.dx.full + g.wgu.full + g.wd.full)), dim3(CX::kThreads), 0, st, g);
+        BPT_HIP(hipGetLastError());
+        return BPT_OK;
+    }
+    // (no rows: products of nothing, zero gradients)
+    if (const int rc = launch_product<false, false, T>(g.wd, b.wd, part, st)) return rc;
+    if (const int rc = launch_product<false, false, T>(g.wgu, b.wgu, part, st)) return rc;
+    // (dX last: it may overwrite dY or X)
+    return s->rows > 0 ? launch_product<true, true, bf16_t>(g.dx, b.dx, part, st) : BPT_OK;
 }
 
 }  // namespace
@@ -631,19 +693,12 @@ int bpt_gated_ffn_bwd(const bpt_gated_ffn_t* s, const void* X, const void* Wg, c
                        : s->activation == BPT_ACT_GELU ? launch_hidden<BPT_ACT_GELU>(h, st) : launch_hidden<BPT_ACT_RELU>(h, st);
         if (rc) return rc;
     }
-    // (no rows: products of nothing, zero gradients)
-    int rc = s->grad_dtype == BPT_BF16 ? weight_grads<bf16_t>(s, b, x, dy, ws, dWg, dWu, dWd, st)
-                                       : weight_grads<float>(s, b, x, dy, ws, dWg, dWu, dWd, st);
-    if (rc || s->rows == 0) return rc;
-    // (dX last: it may overwrite dY or X)
-    ProductArgs g = {};
-    g.A[0] = reinterpret_cast<const bf16_t*>(ws + b.dG); g.A[1] = reinterpret_cast<const bf16_t*>(ws + b.dU);
-    g.B[0] = static_cast<const bf16_t*>(Wg); g.B[1] = static_cast<const bf16_t*>(Wu);
-    g.C[0] = g.C[1] = dX;
-    g.M = s->rows; g.N = s->d; g.K = s->f;
-    g.lda = g.ldb = s->f; g.ldc = s->stride;
-    g.terms = 2; g.matrices = 1;
-    return launch_product<true, true, bf16_t>(g, b.dx, ws + b.part, st);
+    const bf16_t *F = reinterpret_cast<const bf16_t*>(ws + b.F), *dG = reinterpret_cast<const bf16_t*>(ws + b.dG),
+                 *dU = reinterpret_cast<const bf16_t*>(ws + b.dU);
+    GradArgs g = {dx_product(s, dG, dU, static_cast<const bf16_t*>(Wg), static_cast<const bf16_t*>(Wu), dX),
+                  wgu_product(s, x, dG, dU, dWg, dWu), wd_product(s, F, dy, dWd)};
+    const bool dx_alone = dX == dY || dX == X;
+    return s->grad_dtype == BPT_BF16 ? grads<bf16_t>(s, b, g, dx_alone, ws + b.part, st) : grads<float>(s, b, g, dx_alone, ws + b.part, st);
 }
 
 }  // extern "C"
