@@ -424,7 +424,7 @@ typedef struct {
 /* Qr, Kr = Q, K turned by the positions pos[b * pos_stride_b + n] (fp32: whole numbers up to 2^24 and halves up to
  * 2^23 are exact; pos_stride_b = 0 shares N positions among the batch; positions must be finite).  K and Kr may both be
  * NULL.  Qr may be Q itself (and Kr be K) with equal strides; else results must not overlap inputs.  Qr and Kr
- * must not overlap.  B * N < 2^31, H < 65536. */
+ * must not overlap.  pos may start at any entry of an array.  B * N < 2^28, H < 65536. */
 int bpt_rotary(const bpt_rotary_t* s, const float* pos, int64_t pos_stride_b, const void* Q, const void* K, void* Qr,
                void* Kr, void* stream);
 
@@ -485,9 +485,10 @@ typedef enum { BPT_ACT_SILU = 0, BPT_ACT_GELU = 1, BPT_ACT_RELU = 2 } bpt_activa
 /* Gated feed-forward block, bf16:  Y = (act(X Wg) * (X Wu)) Wd  for every row, maps stored as the layer's
  * ([inputs][outputs], y = x W): Wg, Wu [d][f], Wd [f][d], contiguous.  act: SILU g / (1 + exp(-g)), GELU
  * g (1 + erf(g / sqrt 2)) / 2, RELU max(0, g).  Products accumulate in fp32; act(X Wg) * (X Wu) is formed from the
- * fp32 sums and rounded once to bf16, the operand type of the next product, as are its gradients. */
+ * fp32 sums and rounded once to bf16, the operand type of the next product, as are its gradients (for few rows the
+ * forward keeps it in two bf16 parts, 16 bits of it). */
 typedef struct {
-    int64_t rows;           /* < 2^31 */
+    int64_t rows;           /* < 2^31; fewer than 2^23 tiles of 64 rows by 64 of d, and of 128 rows by 128 of f */
     int32_t d, f;           /* multiples of 8, 8 .. 65536 */
     int32_t dtype;          /* BPT_BF16 (BPT_ERR_UNSUPPORTED otherwise) */
     int32_t activation;     /* bpt_activation_t */

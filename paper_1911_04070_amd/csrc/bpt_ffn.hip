@@ -62,7 +62,7 @@ __device__ __forceinline__ void store4(float* p, float a, float b, float c, floa
 // ---- F = act(X Wg) * (X Wu) ---------------------------------------------------------------------------------
 struct UpArgs {
     const bf16_t *X, *Wg, *Wu;
-    bf16_t* F;
+    bf16_t *F, *F_low;    // (F_low: strips only)
     int64_t M, ldx;
     int32_t d, f, tiles_m, tiles_n;
 };
@@ -112,16 +112,18 @@ __device__ __forceinline__ int strip_of(int id, int strips) {
     const int each = strips / kXcds, more = strips % kXcds, xcd = id % kXcds;
     return xcd * each + min(xcd, more) + id / kXcds;
 }
-using UpStrip = Strip<4, 4, true>;
+// F leaves in two bf16 parts, the second what the first's rounding left over: for few rows the second costs nothing that
+// would show (the weights are what is read), and Y is then as good as with F in fp32.
+using UpStrip = Strip<4, 4, 1, 2>;
 template <int ACT>
 __global__ void __launch_bounds__(UpStrip::kThreads) gated_up_strip_kernel(const UpArgs g) {
     __shared__ __attribute__((aligned(1024))) unsigned char shared[UpStrip::kLds];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n0 = strip_of(blockIdx.x, gridDim.x) * 32;
     const int64_t m0 = (int64_t)blockIdx.y * 32;
-    const bf16_t* w[2] = {g.Wg + n0, g.Wu + n0};
+    const bf16_t *x[1] = {g.X + m0 * g.ldx}, *w[2] = {g.Wg + n0, g.Wu + n0};
     float4 sum[2];
-    UpStrip::run(shared, wave, lane, g.X + m0 * g.ldx, g.ldx, g.M - m0, w, g.f, g.f - n0, 0, g.d, sum);
+    UpStrip::run(shared, wave, lane, x, g.ldx, g.M - m0, w, g.f, g.f - n0, g.d, sum);
     const int64_t m = m0 + (lane & 31);
     const int n = n0 + 8 * wave + 4 * (lane >> 5);
     if (wave >= 4 || m >= g.M || n >= g.f) return;
@@ -133,24 +135,34 @@ __global__ void __launch_bounds__(UpStrip::kThreads) gated_up_strip_kernel(const
         activation<ACT>(gate[e], value, slope);
         v[e] = value * up[e];
     }
-    *reinterpret_cast<uint2*>(g.F + m * g.f + n) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+    const uint2 hi = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+    *reinterpret_cast<uint2*>(g.F + m * g.f + n) = hi;
+    if (!g.F_low) return;
+    // (an infinite F has no rest: inf - inf)
+    const float h[4] = {bf16_as_f32(hi.x & 0xFFFFu), __uint_as_float(hi.x & 0xFFFF0000u), bf16_as_f32(hi.y & 0xFFFFu), __uint_as_float(hi.y & 0xFFFF0000u)};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = fabsf(h[e]) < INFINITY ? v[e] - h[e] : 0.f;
+    *reinterpret_cast<uint2*>(g.F_low + m * g.f + n) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
 }
 
 struct DownArgs {
-    const bf16_t *F, *Wd;
+    const bf16_t *F[2], *Wd;
     bf16_t* Y;
     int64_t M, ldy;
     int32_t d, f;
 };
-using DownStrip = Strip<8, 4, false>;
-__global__ void __launch_bounds__(DownStrip::kThreads) down_strip_kernel(const DownArgs g) {
-    __shared__ __attribute__((aligned(1024))) unsigned char shared[DownStrip::kLds];
+template <int PARTS>   // of F
+using DownStrip = Strip<8, PARTS == 2 ? 3 : 4, PARTS, 1>;
+template <int PARTS>
+__global__ void __launch_bounds__(DownStrip<PARTS>::kThreads) down_strip_kernel(const DownArgs g) {
+    using S = DownStrip<PARTS>;
+    __shared__ __attribute__((aligned(1024))) unsigned char shared[S::kLds];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n0 = strip_of(blockIdx.x, gridDim.x) * 32;
     const int64_t m0 = (int64_t)blockIdx.y * 32;
-    const bf16_t* w[1] = {g.Wd + n0};
+    const bf16_t *x[2] = {g.F[0] + m0 * g.f, g.F[1] + m0 * g.f}, *w[1] = {g.Wd + n0};
     float4 sum[1];
-    DownStrip::run(shared, wave, lane, g.F + m0 * g.f, g.f, g.M - m0, w, g.d, g.d - n0, 0, g.f, sum);
+    S::run(shared, wave, lane, x, g.f, g.M - m0, w, g.d, g.d - n0, g.f, sum);
     const int64_t m = m0 + (lane & 31);
     const int n = n0 + 8 * wave + 4 * (lane >> 5);
     if (wave >= 4 || m >= g.M || n >= g.d) return;
@@ -527,21 +539,26 @@ int check_ffn(const bpt_gated_ffn_t* s) {
     if (s->stride < s->d || (s->stride & 7) || s->stride >= ((int64_t)1 << 20)) return BPT_ERR_INVALID_ARG;
     if (s->activation < BPT_ACT_SILU || s->activation > BPT_ACT_RELU) return BPT_ERR_INVALID_ARG;
     if (s->grad_dtype != BPT_F32 && s->grad_dtype != BPT_BF16) return BPT_ERR_INVALID_ARG;
-    // tiles are numbered in 31 bits (of 64 x 64 at least)
-    if (((s->rows + 63) / 64) * ((std::max(s->d, s->f) + 63) / 64) > INT32_MAX) return BPT_ERR_UNSUPPORTED;
+    // a launch has fewer than 2^32 threads, 512 for a tile at most
+    if (((s->rows + 63) / 64) * ((s->d + 63) / 64) >= 1 << 23 || ((s->rows + 127) / 128) * ((s->f + 127) / 128) >= 1 << 23) return BPT_ERR_UNSUPPORTED;
     return BPT_OK;
 }
 
 struct FwdBuffers {
     ProductPlan down;
-    size_t F, part, total;
+    bool up_strips, down_strips;
+    size_t F, F_low, part, total;
 };
 FwdBuffers fwd_buffers(const bpt_gated_ffn_t* s) {
     FwdBuffers b = {};
-    b.down = plan_product(s->rows, s->d, s->f, 1, 1);
+    b.up_strips = use_strips(s->rows, s->f);
+    b.down_strips = use_strips(s->rows, s->d);
+    if (!b.down_strips) b.down = plan_product(s->rows, s->d, s->f, 1, 1);
+    const size_t hidden = align256((size_t)s->rows * s->f * 2);
     b.F = 0;
-    b.part = align256((size_t)s->rows * s->f * 2);
-    b.total = b.part + (use_strips(s->rows, s->d) ? 0 : part_bytes(b.down));
+    b.F_low = hidden;
+    b.part = b.F_low + (b.up_strips && b.down_strips ? hidden : 0);
+    b.total = b.part + (b.down_strips ? 0 : part_bytes(b.down));
     return b;
 }
 struct BwdBuffers {
@@ -649,13 +666,17 @@ int bpt_gated_ffn_fwd(const bpt_gated_ffn_t* s, const void* X, const void* Wg, c
     UpArgs u = {};
     u.X = static_cast<const bf16_t*>(X); u.Wg = static_cast<const bf16_t*>(Wg); u.Wu = static_cast<const bf16_t*>(Wu);
     u.F = F;
+    u.F_low = b.up_strips && b.down_strips ? reinterpret_cast<bf16_t*>(ws + b.F_low) : nullptr;
     u.M = s->rows; u.ldx = s->stride; u.d = s->d; u.f = s->f;
     const int rc = s->activation == BPT_ACT_SILU ? launch_up<BPT_ACT_SILU>(u, st)
                    : s->activation == BPT_ACT_GELU ? launch_up<BPT_ACT_GELU>(u, st) : launch_up<BPT_ACT_RELU>(u, st);
     if (rc) return rc;
-    if (use_strips(s->rows, s->d)) {
-        const DownArgs g = {F, static_cast<const bf16_t*>(Wd), static_cast<bf16_t*>(Y), s->rows, s->stride, s->d, s->f};
-        BPT_LAUNCH("down_strip_kernel", down_strip_kernel, strip_grid(s->rows, s->d), dim3(DownStrip::kThreads), 0, st, g);
+    if (b.down_strips) {
+        const DownArgs g = {{F, u.F_low}, static_cast<const bf16_t*>(Wd), static_cast<bf16_t*>(Y), s->rows, s->stride, s->d, s->f};
+        if (u.F_low)
+            BPT_LAUNCH("down_strip_kernel", down_strip_kernel<2>, strip_grid(s->rows, s->d), dim3(DownStrip<2>::kThreads), 0, st, g);
+        else
+            BPT_LAUNCH("down_strip_kernel", down_strip_kernel<1>, strip_grid(s->rows, s->d), dim3(DownStrip<1>::kThreads), 0, st, g);
         BPT_HIP(hipGetLastError());
         return BPT_OK;
     }

@@ -225,73 +225,82 @@ struct Tile {
         slab_barrier<0>();
     }
 };
-// For few rows: 32 x 32 of C (PAIR: of two products with the same A) in a workgroup, whose WAVES wavefronts each take a
-// part of k with slabs, loads and waits of their own, so that all of them keep loads of the weights in flight; their sums
-// meet in LDS at the end.  A and B as in a Tile with k contiguous in A and n in B.
-template <int WAVES, int STAGES, bool PAIR>
+// For few rows: 32 x 32 of C in a workgroup, whose WAVES wavefronts each take a part of k with slabs, loads and waits of their own,
+// so that all of them keep loads of the weights in flight; their sums meet in LDS at the end.  A and B as in a Tile with k
+// contiguous in A and n in B.  BS = 2: of two products A B[0], A B[1]; AS = 2: of (A[0] + A[1]) B, A in two parts.
+template <int WAVES, int STAGES, int AS, int BS>
 struct Strip {
-    static constexpr int kSlab = 32, kThreads = 64 * WAVES, kMats = PAIR ? 2 : 1;
+    static constexpr int kSlab = 32, kThreads = 64 * WAVES;
     using LoadA = SlabLoader<32, 1, true, kSlab>;
     using LoadB = SlabLoader<32, 1, false, kSlab>;
-    static constexpr int kStage = LoadA::kBytes + kMats * LoadB::kBytes;
-    static constexpr int kPending = LoadA::kLoads + kMats * LoadB::kLoads;
+    static constexpr int kStage = AS * LoadA::kBytes + BS * LoadB::kBytes;
+    static constexpr int kPending = AS * LoadA::kLoads + BS * LoadB::kLoads;
     static constexpr int kLds = WAVES * STAGES * kStage;
-    static_assert(STAGES == 4 && WAVES >= 4 && kLds >= WAVES * kMats * 4096, "waits and the final sums are written for these");
-    typedef f32x16_t Acc[kMats];
+    static_assert((STAGES == 3 || STAGES == 4) && WAVES >= 4 && kLds >= WAVES * BS * 4096 && kLds <= 160 * 1024,
+                  "waits and the final sums are written for these");
 
     // On return wavefront w < 4 holds in sum[mat] C[lane % 32][8 w + 4 (lane / 32) ..+ 3].  a: first row's k = 0; b: first column's.
-    static __device__ __forceinline__ void run(unsigned char* shared, int wave, int lane, const bf16_t* a, int64_t lda, int64_t rows,
-                                               const bf16_t* const* b, int64_t ldb, int cols, int64_t k_from, int64_t k_to, float4* sum) {
+    static __device__ __forceinline__ void run(unsigned char* shared, int wave, int lane, const bf16_t* const* a, int64_t lda, int64_t rows,
+                                               const bf16_t* const* b, int64_t ldb, int cols, int k_all, float4* sum) {
         lds_bytes_t all = (lds_bytes_t)shared, mine = all + wave * STAGES * kStage;
         LoadA la;
         LoadB lb;
         la.init(0, lane, lda, rows);
         lb.init(0, lane, ldb, cols);
-        const int slabs = (int)((k_to - k_from + kSlab - 1) / kSlab), each = (slabs + WAVES - 1) / WAVES;
-        const int count = max(min(each, slabs - wave * each), 0);
-        const int64_t k0 = k_from + (int64_t)wave * each * kSlab;
-        auto load = [&](int t) {
-            const int64_t k = k0 + (int64_t)t * kSlab;
-            lds_bytes_t p = mine + (t & (STAGES - 1)) * kStage;
-            la.load(a + k, k_to - k, p, 0, lane);
+        const int slabs = (k_all + kSlab - 1) / kSlab, each = (slabs + WAVES - 1) / WAVES;
+        const int count = max(min(each, slabs - wave * each), 0), k0 = wave * each * kSlab;
+        auto load = [&](int t, int stage) {
+            const int k = k0 + t * kSlab;
+            lds_bytes_t p = mine + stage * kStage;
 #pragma unroll
-            for (int m = 0; m < kMats; ++m) lb.load(b[m] + k * ldb, k_to - k, p + LoadA::kBytes + m * LoadB::kBytes, 0, lane);
+            for (int m = 0; m < AS; ++m) la.load(a[m] + k, k_all - k, p + m * LoadA::kBytes, 0, lane);
+#pragma unroll
+            for (int m = 0; m < BS; ++m) lb.load(b[m] + (int64_t)k * ldb, k_all - k, p + AS * LoadA::kBytes + m * LoadB::kBytes, 0, lane);
         };
-        Acc acc = {};
-        for (int t = 0; t < min(STAGES - 1, count); ++t) load(t);
+        f32x16_t acc[BS] = {};
+#pragma unroll
+        for (int t = 0; t < STAGES - 1; ++t)
+            if (t < count) load(t, t);
+        int stage = 0, next = STAGES - 1;
         for (int t = 0; t < count; ++t) {
             // this slab has arrived (those behind it may be on their way), and the reads of the one before are through
-            const int behind = count - 1 - t;
-            if (behind >= 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(2 * kPending) : "memory");
+            const int behind = min(STAGES - 2, count - 1 - t);
+            if (STAGES > 3 && behind == 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(2 * kPending) : "memory");
             else if (behind == 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(kPending) : "memory");
             else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-            if (t + STAGES - 1 < count) load(t + STAGES - 1);
-            lds_bytes_t p = mine + (t & (STAGES - 1)) * kStage;
+            if (t + STAGES - 1 < count) load(t + STAGES - 1, next);
+            lds_bytes_t pa = mine + stage * kStage, pb = pa + AS * LoadA::kBytes;
 #pragma unroll
             for (int kk = 0; kk < kSlab / 16; ++kk) {
-                const bf16x8_t x = fragment<32, true, kSlab>(p, 0, kk, lane);
+                bf16x8_t x[AS], y[BS];
 #pragma unroll
-                for (int m = 0; m < kMats; ++m)
-                    acc[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fragment<32, false, kSlab>(p + LoadA::kBytes + m * LoadB::kBytes, 0, kk, lane), x,
-                                                                     acc[m], 0, 0, 0);
+                for (int m = 0; m < AS; ++m) x[m] = fragment<32, true, kSlab>(pa + m * LoadA::kBytes, 0, kk, lane);
+#pragma unroll
+                for (int m = 0; m < BS; ++m) y[m] = fragment<32, false, kSlab>(pb + m * LoadB::kBytes, 0, kk, lane);
+#pragma unroll
+                for (int u = 0; u < AS; ++u)
+#pragma unroll
+                    for (int m = 0; m < BS; ++m) acc[m] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y[m], x[u], acc[m], 0, 0, 0);
             }
+            stage = stage + 1 == STAGES ? 0 : stage + 1;
+            next = next + 1 == STAGES ? 0 : next + 1;
         }
         slab_barrier<0>();   // (the sums take the slabs' place)
         typedef __attribute__((address_space(3))) f32x4_t* ptr_t;
 #pragma unroll
-        for (int m = 0; m < kMats; ++m)
+        for (int m = 0; m < BS; ++m)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const f32x4_t v = {acc[m][4 * q], acc[m][4 * q + 1], acc[m][4 * q + 2], acc[m][4 * q + 3]};
-                *(ptr_t)(all + ((wave * kMats + m) * 4 + q) * 1024 + lane * 16) = v;
+                *(ptr_t)(all + ((wave * BS + m) * 4 + q) * 1024 + lane * 16) = v;
             }
         __syncthreads();
         if (wave < 4)
 #pragma unroll
-            for (int m = 0; m < kMats; ++m) {
+            for (int m = 0; m < BS; ++m) {
                 f32x4_t v = {};
 #pragma unroll
-                for (int w = 0; w < WAVES; ++w) v += *(ptr_t)(all + ((w * kMats + m) * 4 + wave) * 1024 + lane * 16);
+                for (int w = 0; w < WAVES; ++w) v += *(ptr_t)(all + ((w * BS + m) * 4 + wave) * 1024 + lane * 16);
                 sum[m] = make_float4(v[0], v[1], v[2], v[3]);
             }
     }

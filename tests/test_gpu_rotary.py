@@ -93,6 +93,13 @@ def test_rotary_in_place_with_strides_and_few_or_many_rows():
             check(want[0], ref, size, dtype)
 
 
+def test_rotary_positions_from_the_middle_of_an_array():
+    Q = make(2, 2, 13, torch.bfloat16, "heads", 4)
+    pos = torch.arange(100, dtype=torch.float32, device="cuda")
+    got, _ = bpt.bpt_rotary(Q, None, pos[37:50])
+    check(got, *reference(Q, pos[37:50], 64, False, 10000.0, 1.0, 0, 1.0, 32.0, False), torch.bfloat16)
+
+
 def test_rotary_writes_its_rows_only_and_takes_broadcast_inputs():
     frame = torch.full((2, 3, 12, 72), 7.0, device="cuda")
     out = frame[:, :2, 1:11, 8:]
