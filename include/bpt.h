@@ -424,7 +424,7 @@ typedef struct {
 /* Qr, Kr = Q, K turned by the positions pos[b * pos_stride_b + n] (fp32: whole numbers up to 2^24 and halves up to
  * 2^23 are exact; pos_stride_b = 0 shares N positions among the batch; positions must be finite).  K and Kr may both be
  * NULL.  Qr may be Q itself (and Kr be K) with equal strides; else results must not overlap inputs.  Qr and Kr
- * must not overlap.  pos may start at any entry of an array.  B * N < 2^28, H < 65536. */
+ * must not overlap.  pos may start at any entry of an array.  B * N <= 2^28 - 32, H < 65536. */
 int bpt_rotary(const bpt_rotary_t* s, const float* pos, int64_t pos_stride_b, const void* Q, const void* K, void* Qr,
                void* Kr, void* stream);
 

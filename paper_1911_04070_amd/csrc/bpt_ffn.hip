@@ -604,13 +604,13 @@ ProductArgs dx_product(const bpt_gated_ffn_t* s, const bf16_t* dG, const bf16_t*
     return g;
 }
 
-// whole tiles of 64 x 64 of all three products in one launch, where that is estimated shorter than the three one by one
-bool plan_together(const BwdBuffers& b, GradArgs& g) {
-    const TileCost& t = kTileCost[kSmall];
+// whole tiles of all three products in one launch, where that is estimated shorter than the three one by one
+float plan_together(GradArgs& g, TileSize size) {
+    const TileCost& t = kTileCost[size];
     int64_t groups = 0, longest = 0, work = 0;
     for (ProductArgs* p : {&g.dx, &g.wgu, &g.wd}) {
         const int64_t slabs = (p->K + t.slab - 1) / t.slab * p->terms, tm = (p->M + t.m - 1) / t.m, tn = (p->N + t.n - 1) / t.n;
-        if (tm * tn * p->matrices > 1 << 20) return false;
+        if (tm * tn * p->matrices > 1 << 20) return INFINITY;
         p->tiles_m = (int)tm;
         p->tiles_n = (int)tn;
         p->full = (int)(tm * tn * p->matrices);
@@ -620,19 +620,26 @@ bool plan_together(const BwdBuffers& b, GradArgs& g) {
         longest = std::max(longest, slabs);
         work += p->full * slabs;
     }
-    const float us = groups <= kCus ? t.us_alone : t.us;
-    const float together = kStartUs + us * std::max((float)longest, (float)work / (kCus * t.per_cu));
-    return together < b.dx.us + b.wgu.us + b.wd.us;
+    if (groups <= kCus) return kStartUs + t.us_alone * (float)longest;
+    const int64_t slots = (int64_t)kCus * t.per_cu, rounds = (groups + slots - 1) / slots;
+    return kStartUs + t.us * std::max((float)longest, (float)(rounds * work) / (float)groups);
+}
+
+template <typename CX, typename CW, typename T>
+int launch_grads(const GradArgs& g, hipStream_t st) {
+    BPT_LAUNCH("grads_kernel", (grads_kernel<CX, CW, T>), dim3((unsigned)(g.dx.full + g.wgu.full + g.wd.full)), dim3(CX::kThreads), 0, st, g);
+    BPT_HIP(hipGetLastError());
+    return BPT_OK;
 }
 
 template <typename T>
 int grads(const bpt_gated_ffn_t* s, const BwdBuffers& b, GradArgs& g, bool dx_alone, void* part, hipStream_t st) {
-    if (s->rows > 0 && !dx_alone && plan_together(b, g)) {
-        using CX = Tile<64, 64, 2, 2, 64, 4, true, true, false>;
-        using CW = Tile<64, 64, 2, 2, 64, 4, false, false, false>;
-        BPT_LAUNCH("grads_kernel", (grads_kernel<CX, CW, T>), dim3((unsigned)(g.dx.full + g.wgu.full + g.wd.full)), dim3(CX::kThreads), 0, st, g);
-        BPT_HIP(hipGetLastError());
-        return BPT_OK;
+    if (s->rows > 0 && !dx_alone) {
+        GradArgs mid = g, small = g;
+        const float us_mid = plan_together(mid, kMid), us_small = plan_together(small, kSmall);
+        if (std::min(us_mid, us_small) < b.dx.us + b.wgu.us + b.wd.us)
+            return us_mid < us_small ? launch_grads<Tile<128, 128, 2, 2, 64, 2, true, true, false>, Tile<128, 128, 2, 2, 64, 2, false, false, false>, T>(mid, st)
+                                     : launch_grads<Tile<64, 64, 2, 2, 64, 4, true, true, false>, Tile<64, 64, 2, 2, 64, 4, false, false, false>, T>(small, st);
     }
     // (no rows: products of nothing, zero gradients)
     if (const int rc = launch_product<false, false, T>(g.wd, b.wd, part, st)) return rc;

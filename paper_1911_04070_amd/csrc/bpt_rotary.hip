@@ -220,7 +220,7 @@ int bpt_rotary(const bpt_rotary_t* s, const float* pos, int64_t pos_stride_b, co
         !std::isfinite(high - low) || std::isnan(s->base) || std::isnan(s->factor) || pos_stride_b < 0)
         return BPT_ERR_INVALID_ARG;
     const int64_t rows = (int64_t)s->B * s->N;
-    if (rows >= 1 << 28 || s->H > 65535) return BPT_ERR_UNSUPPORTED;   // a launch has fewer than 2^32 threads, 256 for 16 rows
+    if (rows > (1 << 28) - 32 || s->H > 65535) return BPT_ERR_UNSUPPORTED;   // a launch has fewer than 2^32 threads, 256 for 16 rows
     if (rows == 0 || s->H == 0) return BPT_OK;
     if (!pos || !Q || !Qr || !K != !Kr || (reinterpret_cast<uintptr_t>(pos) & 3) || off_boundary(Q, K, Qr, Kr) || Qr == Kr) return BPT_ERR_INVALID_ARG;
     if (!rows_apart(s->B, s->H, s->N, out[0], out[1], out[2])) return BPT_ERR_INVALID_ARG;
