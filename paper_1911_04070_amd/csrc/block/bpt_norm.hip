@@ -20,7 +20,7 @@ struct NormArgs {
     const float4* stats;
     void *y, *h, *dx, *d_branch;
     float4* stats_out;
-    void* d_gate;          // written by the row kernel where gate_direct, else by the sum over slices
+    void* d_gate;          // written by the row kernel where a gate row has one slice, else by the sum over slices
     float* gate_part;      // [units][d]: sums of a slice of a gate row's rows
     float* part;           // [gridDim.x][sums][d]: sums over a workgroup's rows
     int64_t rows, stride, gate_rows;
@@ -97,7 +97,9 @@ __device__ __forceinline__ void params8(const float* p, int col, bool has, float
 }
 
 // Bound by HBM: x and branch in, y and h out, the row in registers in between; parameters of a thread's columns stay in
-// registers, the next row is loaded before the current one's sums are exchanged.
+// registers, the next row is loaded before the current one's sums are exchanged.  65 532 rows of 512 in bf16, a gate row for every
+// 16 383: 49 us, 5.5 TB/s (a large copy reaches 4.9 on the same device; part of what it moves is still in the memory-side
+// cache); 4095 rows of 2048 in fp32: 33 us, 4.1 TB/s.
 template <typename T, int THREADS>
 __global__ void __launch_bounds__(RowTeam<THREADS>::kBlock) residual_norm_kernel(const NormArgs a) {
     using Team = RowTeam<THREADS>;
@@ -157,7 +159,8 @@ __global__ void __launch_bounds__(RowTeam<THREADS>::kBlock) residual_norm_kernel
 //   d_branch = rb (s - [layer] mean(s) - bhat mean(s bhat)),  s = dN g1
 // and column sums dN bhat, dN, dh yhat, dh for gains and biases.  x and branch are read again (y is formed from them in
 // fp32 as the forward did, not from its rounded copy), six values of memory traffic per element; the sums stay in the
-// thread's registers over all rows of its workgroup.
+// thread's registers over all rows of its workgroup, which leaves two wavefronts per SIMD: rows have to be requested early.
+// 65 532 rows of 512 in bf16: 93 us, 4.3 TB/s (one row ahead instead of two: 100 us); 4095 rows of 2048 in fp32: 40 us, 5.0 TB/s.
 template <typename T, int THREADS>
 __global__ void __launch_bounds__(RowTeam<THREADS>::kBlock, 2) residual_norm_bwd_kernel(const NormArgs a) {
     using Team = RowTeam<THREADS>;
@@ -318,7 +321,7 @@ __global__ void __launch_bounds__(RowTeam<THREADS>::kBlock, 2) residual_norm_bwd
 
 // Column sums of up to 4 + gate rows of tables: job j < num_sums adds `parts` rows of part, `num_sums` rows apart; job
 // num_sums + g adds the `slices` rows of gate row g.  A workgroup takes 32 columns, 8 lanes of 16 bytes per row, 32 rows
-// in flight; sums are added across lanes and wavefronts in a fixed tree.
+// in flight; sums are added across lanes and wavefronts in a fixed tree.  512 rows of 2 x 512 and 4 x 128 of 512: 5 us.
 struct SumJobs {
     const float *part, *gate_part;
     float* out[4];
