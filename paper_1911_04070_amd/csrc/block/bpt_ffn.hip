@@ -149,11 +149,13 @@ __global__ void __launch_bounds__(UpStrip::kThreads) gated_up_strip_kernel(const
     *reinterpret_cast<uint2*>(g.F_low + m * g.f + n) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
 }
 
+// (blockIdx.z: a slice of k, where the strips leave most of the device idle; its sums go to `part` and are added in order)
 struct DownArgs {
     const bf16_t *F[2], *Wd;
     bf16_t* Y;
     int64_t M, ldy;
-    int32_t d, f;
+    int32_t d, f, slices, slice_k;
+    float* part;          // [slice][M][d]
 };
 template <int PARTS>   // of F
 using DownStrip = Strip<8, PARTS == 2 ? 3 : 4, PARTS, 1>;
@@ -164,13 +166,27 @@ __global__ void __launch_bounds__(DownStrip<PARTS>::kThreads) down_strip_kernel(
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n0 = strip_of(blockIdx.x, gridDim.x) * 32;
     const int64_t m0 = (int64_t)blockIdx.y * 32;
-    const bf16_t *x[2] = {g.F[0] + m0 * g.f, g.F[1] + m0 * g.f}, *w[1] = {g.Wd + n0};
+    const int k0 = blockIdx.z * g.slice_k;
+    const bf16_t *x[2] = {g.F[0] + m0 * g.f + k0, PARTS == 2 ? g.F[1] + m0 * g.f + k0 : nullptr}, *w[1] = {g.Wd + (int64_t)k0 * g.d + n0};
     float4 sum[1];
-    S::run(shared, wave, lane, x, g.f, g.M - m0, w, g.d, g.d - n0, g.f, sum);
+    S::run(shared, wave, lane, x, g.f, g.M - m0, w, g.d, g.d - n0, min(g.slice_k, g.f - k0), sum);
     const int64_t m = m0 + (lane & 31);
     const int n = n0 + 8 * wave + 4 * (lane >> 5);
     if (wave >= 4 || m >= g.M || n >= g.d) return;
-    *reinterpret_cast<uint2*>(g.Y + m * g.ldy + n) = make_uint2(bf16_pair(sum[0].x, sum[0].y), bf16_pair(sum[0].z, sum[0].w));
+    if (g.slices > 1) store4(g.part + ((int64_t)blockIdx.z * g.M + m) * g.d + n, sum[0].x, sum[0].y, sum[0].z, sum[0].w);
+    else *reinterpret_cast<uint2*>(g.Y + m * g.ldy + n) = make_uint2(bf16_pair(sum[0].x, sum[0].y), bf16_pair(sum[0].z, sum[0].w));
+}
+__global__ void __launch_bounds__(256) down_sum_kernel(const DownArgs g) {
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, elems = g.M * g.d;
+    if (i >= elems) return;
+    float4 x = *reinterpret_cast<const float4*>(g.part + i);
+#pragma unroll 4
+    for (int s = 1; s < g.slices; ++s) {
+        const float4 v = *reinterpret_cast<const float4*>(g.part + s * elems + i);
+        x.x += v.x; x.y += v.y; x.z += v.z; x.w += v.w;
+    }
+    const int64_t m = i / g.d;
+    *reinterpret_cast<uint2*>(g.Y + m * g.ldy + (i - m * g.d)) = make_uint2(bf16_pair(x.x, x.y), bf16_pair(x.z, x.w));
 }
 
 // ---- C = A0 B0 (+ A1 B1), or several products side by side ------------------------------------------------------
@@ -265,17 +281,20 @@ __global__ void __launch_bounds__(C::kThreads, C::kWavesPerSimd) product_kernel(
     product_body<C, A_KFIRST, B_KFIRST, T>(g, blockIdx.x, shared);
 }
 
-// The three products of the backward at once, dX (the longest sums) first: for few rows none of them fills the device.
+// The three products of the backward at once, the longest sums first: for few rows none of them fills the device.
 struct GradArgs {
     ProductArgs dx, wgu, wd;   // whole tiles only
+    int32_t dx_last;
 };
 template <typename CX, typename CW, typename T>
 __global__ void __launch_bounds__(CX::kThreads, CX::kWavesPerSimd) grads_kernel(const GradArgs g) {
     static_assert(CX::kThreads == CW::kThreads && CX::kLds == CW::kLds, "one launch");
     __shared__ __attribute__((aligned(1024))) unsigned char shared[CX::kLds];
-    const int group = blockIdx.x, wgu = group - g.dx.full, wd = wgu - g.wgu.full;
-    if (wgu < 0) return product_body<CX, true, true, bf16_t>(g.dx, group, shared);
-    product_body<CW, false, false, T>(wd < 0 ? g.wgu : g.wd, wd < 0 ? wgu : wd, shared);
+    const int weights = g.wgu.full + g.wd.full, group = blockIdx.x;
+    const int dx = g.dx_last ? group - weights : group, w = g.dx_last ? group : group - g.dx.full;
+    if (g.dx_last ? dx >= 0 : w < 0) return product_body<CX, true, true, bf16_t>(g.dx, dx, shared);
+    const int wd = w - g.wgu.full;
+    product_body<CW, false, false, T>(wd < 0 ? g.wgu : g.wd, wd < 0 ? w : wd, shared);
 }
 
 // The left-over tiles: sums of their slices in order; a workgroup takes one 32 x 32 block of each wavefront.
@@ -409,9 +428,14 @@ constexpr int kCus = 256;
 enum TileSize { kBig, kWide, kMid, kSmall };
 struct TileCost {
     int m, n, slab, per_cu;
-    float us, us_alone;   // of 64 k, all compute units busy; and with at most one workgroup on each
+    float us, us_one, us_few;   // of 64 k: the device full; one workgroup on every compute unit; few compute units busy
 };
-constexpr TileCost kTileCost[] = {{256, 256, 64, 1, 2.1f, 2.1f}, {128, 256, 32, 2, 2.35f, 1.5f}, {128, 128, 64, 2, 1.25f, 0.68f}, {64, 64, 64, 2, 0.53f, 0.40f}};
+constexpr TileCost kTileCost[] = {{256, 256, 64, 1, 2.1f, 2.1f, 1.45f}, {128, 256, 32, 2, 2.35f, 1.7f, 1.15f}, {128, 128, 64, 2, 1.25f, 0.92f, 0.60f},
+                                  {64, 64, 64, 2, 0.53f, 0.43f, 0.37f}};
+float slab_us(const TileCost& t, int64_t groups) {   // in between, in proportion
+    if (groups <= kCus) return t.us_few + (t.us_one - t.us_few) * (float)groups / kCus;
+    return t.us_one + (t.us - t.us_one) * std::min(1.f, (float)(groups - kCus) / kCus);
+}
 constexpr float kStartUs = 2.5f;             // a tile's first loads and its results
 constexpr float kSumUs = 3.5f, kSumBytesPerUs = 5.0e6f;   // adding up slices: a launch, and their bytes written and read
 constexpr int kMaxSlices = 32, kMinSliceK = 128;
@@ -435,9 +459,8 @@ ProductPlan plan_product(int64_t M, int64_t N, int64_t K, int terms, int matrice
         const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * matrices, slots = (int64_t)kCus * t.per_cu;
         const int64_t slabs = (K + t.slab - 1) / t.slab * terms;
         auto rounds = [&](int64_t groups, int64_t n) {   // of workgroups with n slabs each
-            const float k = (float)n * t.slab / 64;
-            if (groups <= kCus) return k * t.us_alone + kStartUs;
-            return (float)((groups + slots - 1) / slots) * (k * t.us + kStartUs);
+            const float one = (float)n * t.slab / 64 * slab_us(t, groups) + kStartUs;
+            return groups <= kCus ? one : (float)((groups + slots - 1) / slots) * one;
         };
         for (int64_t s = 1; s <= kMaxSlices && (s == 1 || slabs * t.slab / s >= kMinSliceK); ++s) {
             const int64_t over = s == 1 ? 0 : tiles % slots;
@@ -554,9 +577,18 @@ int check_ffn(const bpt_gated_ffn_t* s) {
     return BPT_OK;
 }
 
+// Slices of k for the strips of the second product: a compute unit takes in about 50 KB a microsecond, its columns of Wd and all of F's
+// rows; with few strips the others help, for the price of a launch that adds the slices.
+int down_slices(int64_t rows, int d, int f, int parts) {
+    const int64_t strips = ((rows + 31) / 32) * ((d + 31) / 32), slices = std::min<int64_t>(kCus / strips, f / 512);
+    const float us = (float)f * 2 * (32 + (float)(parts * std::min<int64_t>(rows, 32))) / 50e3f;
+    return slices > 1 && us * (1.f - 1.f / (float)slices) > kSumUs + 1.f ? (int)slices : 1;
+}
+
 struct FwdBuffers {
     ProductPlan down;
     bool up_strips, down_strips;
+    int slices, slice_k;      // of the strips
     size_t F, F_low, part, total;
 };
 FwdBuffers fwd_buffers(const bpt_gated_ffn_t* s) {
@@ -567,8 +599,14 @@ FwdBuffers fwd_buffers(const bpt_gated_ffn_t* s) {
     const size_t hidden = align256((size_t)s->rows * s->f * 2);
     b.F = 0;
     b.F_low = hidden;
-    b.part = b.F_low + (b.up_strips && b.down_strips ? hidden : 0);
-    b.total = b.part + (b.down_strips ? 0 : part_bytes(b.down));
+    const bool two_parts = b.up_strips && b.down_strips;
+    b.part = b.F_low + (two_parts ? hidden : 0);
+    if (b.down_strips) {
+        b.slices = down_slices(std::max<int64_t>(s->rows, 1), s->d, s->f, two_parts ? 2 : 1);
+        b.slice_k = ((s->f + b.slices - 1) / b.slices + 31) / 32 * 32;
+        b.slices = (s->f + b.slice_k - 1) / b.slice_k;
+    }
+    b.total = b.part + (b.down_strips ? (b.slices > 1 ? align256((size_t)b.slices * s->rows * s->d * 4) : 0) : part_bytes(b.down));
     return b;
 }
 struct BwdBuffers {
@@ -614,25 +652,34 @@ ProductArgs dx_product(const bpt_gated_ffn_t* s, const bf16_t* dG, const bf16_t*
     return g;
 }
 
-// whole tiles of all three products in one launch, where that is estimated shorter than the three one by one
-float plan_together(GradArgs& g, TileSize size) {
-    const TileCost& t = kTileCost[size];
-    int64_t groups = 0, longest = 0, work = 0;
-    for (ProductArgs* p : {&g.dx, &g.wgu, &g.wd}) {
-        const int64_t slabs = (p->K + t.slab - 1) / t.slab * p->terms, tm = (p->M + t.m - 1) / t.m, tn = (p->N + t.n - 1) / t.n;
-        if (tm * tn * p->matrices > 1 << 20) return INFINITY;
-        p->tiles_m = (int)tm;
-        p->tiles_n = (int)tn;
-        p->full = (int)(tm * tn * p->matrices);
-        p->slices = 1;
-        p->slice_slabs = (int)slabs;
-        groups += p->full;
-        longest = std::max(longest, slabs);
-        work += p->full * slabs;
+// whole tiles of all three products in one launch, dX in one size and the weights' gradients in another, where that is estimated
+// shorter than the three one by one
+float plan_together(GradArgs& g, TileSize x, TileSize w) {
+    ProductArgs* const product[3] = {&g.dx, &g.wgu, &g.wd};
+    int64_t groups = 0, slabs[3];
+    for (int i = 0; i < 3; ++i) {
+        ProductArgs& p = *product[i];
+        const TileCost& t = kTileCost[i == 0 ? x : w];
+        const int64_t tm = (p.M + t.m - 1) / t.m, tn = (p.N + t.n - 1) / t.n;
+        if (tm * tn * p.matrices > 1 << 20) return INFINITY;
+        slabs[i] = (p.K + t.slab - 1) / t.slab * p.terms;
+        p.tiles_m = (int)tm;
+        p.tiles_n = (int)tn;
+        p.full = (int)(tm * tn * p.matrices);
+        p.slices = 1;
+        p.slice_slabs = (int)slabs[i];
+        groups += p.full;
     }
-    if (groups <= kCus) return kStartUs + t.us_alone * (float)longest;
-    const int64_t slots = (int64_t)kCus * t.per_cu, rounds = (groups + slots - 1) / slots;
-    return kStartUs + t.us * std::max((float)longest, (float)(rounds * work) / (float)groups);
+    float longest = 0.f, work = 0.f;
+    for (int i = 0; i < 3; ++i) {
+        const float us = (float)slabs[i] * slab_us(kTileCost[i == 0 ? x : w], groups);
+        longest = std::max(longest, us);
+        work += (float)product[i]->full * us;
+    }
+    g.dx_last = slabs[0] < slabs[1];
+    if (groups <= 2 * kCus) return kStartUs + longest;   // (two of either size per compute unit)
+    // several rounds of unequal lengths: measured up to a quarter over their mean
+    return kStartUs + 1.25f * std::max(longest, work / (2 * kCus));
 }
 
 template <typename CX, typename CW, typename T>
@@ -645,11 +692,25 @@ int launch_grads(const GradArgs& g, hipStream_t st) {
 template <typename T>
 int grads(const bpt_gated_ffn_t* s, const BwdBuffers& b, GradArgs& g, bool dx_alone, void* part, hipStream_t st) {
     if (s->rows > 0 && !dx_alone) {
-        GradArgs mid = g, small = g;
-        const float us_mid = plan_together(mid, kMid), us_small = plan_together(small, kSmall);
-        if (std::min(us_mid, us_small) < b.dx.us + b.wgu.us + b.wd.us)
-            return us_mid < us_small ? launch_grads<Tile<128, 128, 2, 2, 64, 2, true, true, false>, Tile<128, 128, 2, 2, 64, 2, false, false, false>, T>(mid, st)
-                                     : launch_grads<Tile<64, 64, 2, 2, 64, 4, true, true, false>, Tile<64, 64, 2, 2, 64, 4, false, false, false>, T>(small, st);
+        GradArgs best = g;
+        float us = b.dx.us + b.wgu.us + b.wd.us;
+        TileSize size[2] = {kBig, kBig};
+        for (TileSize x : {kMid, kSmall})
+            for (TileSize w : {kMid, kSmall}) {
+                GradArgs a = g;
+                const float t = plan_together(a, x, w);
+                if (t >= us) continue;
+                us = t;
+                best = a;
+                size[0] = x;
+                size[1] = w;
+            }
+        using MidX = Tile<128, 128, 2, 2, 64, 2, true, true, false>;
+        using MidW = Tile<128, 128, 2, 2, 64, 2, false, false, false>;
+        using SmallX = Tile<64, 64, 2, 2, 64, 4, true, true, false>;
+        using SmallW = Tile<64, 64, 2, 2, 64, 4, false, false, false>;
+        if (size[0] == kMid) return size[1] == kMid ? launch_grads<MidX, MidW, T>(best, st) : launch_grads<MidX, SmallW, T>(best, st);
+        if (size[0] == kSmall) return size[1] == kMid ? launch_grads<SmallX, MidW, T>(best, st) : launch_grads<SmallX, SmallW, T>(best, st);
     }
     // (no rows: products of nothing, zero gradients)
     if (const int rc = launch_product<false, false, T>(g.wd, b.wd, part, st)) return rc;
@@ -689,12 +750,19 @@ int bpt_gated_ffn_fwd(const bpt_gated_ffn_t* s, const void* X, const void* Wg, c
                    : s->activation == BPT_ACT_GELU ? launch_up<BPT_ACT_GELU>(u, st) : launch_up<BPT_ACT_RELU>(u, st);
     if (rc) return rc;
     if (b.down_strips) {
-        const DownArgs g = {{F, u.F_low}, static_cast<const bf16_t*>(Wd), static_cast<bf16_t*>(Y), s->rows, s->stride, s->d, s->f};
+        const DownArgs g = {{F, u.F_low}, static_cast<const bf16_t*>(Wd), static_cast<bf16_t*>(Y), s->rows, s->stride, s->d, s->f, b.slices, b.slice_k,
+                            reinterpret_cast<float*>(ws + b.part)};
+        dim3 grid = strip_grid(s->rows, s->d);
+        grid.z = b.slices;
         if (u.F_low)
-            BPT_LAUNCH("down_strip_kernel", down_strip_kernel<2>, strip_grid(s->rows, s->d), dim3(DownStrip<2>::kThreads), 0, st, g);
+            BPT_LAUNCH("down_strip_kernel", down_strip_kernel<2>, grid, dim3(DownStrip<2>::kThreads), 0, st, g);
         else
-            BPT_LAUNCH("down_strip_kernel", down_strip_kernel<1>, strip_grid(s->rows, s->d), dim3(DownStrip<1>::kThreads), 0, st, g);
+            BPT_LAUNCH("down_strip_kernel", down_strip_kernel<1>, grid, dim3(DownStrip<1>::kThreads), 0, st, g);
         BPT_HIP(hipGetLastError());
+        if (b.slices > 1) {
+            BPT_LAUNCH("down_sum_kernel", down_sum_kernel, dim3((unsigned)((s->rows * s->d / 4 + 255) / 256)), dim3(256), 0, st, g);
+            BPT_HIP(hipGetLastError());
+        }
         return BPT_OK;
     }
     ProductArgs g = {};
@@ -734,7 +802,7 @@ int bpt_gated_ffn_bwd(const bpt_gated_ffn_t* s, const void* X, const void* Wg, c
     const bf16_t *F = reinterpret_cast<const bf16_t*>(ws + b.F), *dG = reinterpret_cast<const bf16_t*>(ws + b.dG),
                  *dU = reinterpret_cast<const bf16_t*>(ws + b.dU);
     GradArgs g = {dx_product(s, dG, dU, static_cast<const bf16_t*>(Wg), static_cast<const bf16_t*>(Wu), dX),
-                  wgu_product(s, x, dG, dU, dWg, dWu), wd_product(s, F, dy, dWd)};
+                  wgu_product(s, x, dG, dU, dWg, dWu), wd_product(s, F, dy, dWd), 0};
     const bool dx_alone = dX == dY || dX == X;
     return s->grad_dtype == BPT_BF16 ? grads<bf16_t>(s, b, g, dx_alone, ws + b.part, st) : grads<float>(s, b, g, dx_alone, ws + b.part, st);
 }
