@@ -11,9 +11,11 @@
 namespace bpt {
 namespace {
 
-// A row is worked on by THREADS threads, 8 consecutive features each: the smallest of 16, 32, 64 (part of a wavefront),
-// 128, 256, 512 (2 to 8 wavefronts) that covers d, so that the row stays in registers between its passes whatever
-// d is; a workgroup of 256 threads (or THREADS) works on several rows side by side.
+// A row is worked on by THREADS threads, 8 consecutive features each: the smallest of 8, 16, 32 (part of a wavefront),
+// 64, 128, 256, 512 (1 to 8 wavefronts) that covers d, so that the row stays in registers between its passes whatever d is; a
+// workgroup of 256 threads (or THREADS) works on several rows side by side.  (Other multiples of 64 leave fewer threads idle and
+// compute units worse filled: 30 000 rows of 1032 in bf16, backward with 192 threads 183 us, with 256 131 us.  500 000 rows of 64 in
+// bf16 with 16 threads a row: forward 70 us, with its backward 199 us; with 8: 44 and 143 us.)
 struct NormArgs {
     const void *x, *branch, *gate, *dy, *dh;
     const float *post_gain, *post_bias, *pre_gain, *pre_bias;
@@ -101,7 +103,7 @@ __device__ __forceinline__ void params8(const float* p, int col, bool has, float
 // 16 383: 49 us, 5.5 TB/s (a large copy reaches 4.9 on the same device; part of what it moves is still in the memory-side
 // cache); 4095 rows of 2048 in fp32: 33 us, 4.1 TB/s.
 template <typename T, int THREADS>
-__global__ void __launch_bounds__(RowTeam<THREADS>::kBlock) residual_norm_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(RowTeam<THREADS>::kBlock, sizeof(T) == 2 ? 5 : 4) residual_norm_kernel(const NormArgs a) {
     using Team = RowTeam<THREADS>;
     __shared__ float2 lds[2 * Team::kBlock / 64];
     int slot = 0;
@@ -367,11 +369,11 @@ __global__ void __launch_bounds__(256) norm_column_sum_kernel(const SumJobs a) {
     }
 }
 
-// compute units; workgroups of 256 threads that are resident on one: forward 5 (bf16) and 4 (fp32), backward 2
-constexpr int kNormBlocks = 256, kNormBwdBlocks = 2 * 256;
+// compute units; wavefronts per SIMD: forward 5 (bf16) and 4 (fp32), backward 2, as the kernels' launch bounds say
+constexpr int kNormCus = 256, kNormBwdBlocks = 2 * 256;
 
 int norm_threads(int d) {
-    int t = 16;
+    int t = 8;
     while (t * 8 < d) t *= 2;
     return t;
 }
@@ -401,7 +403,16 @@ BwdPlan bwd_plan(const bpt_residual_norm_t* s) {
     const bool shared_gate = s->gate_rows > 1;
     p.group_rows = shared_gate ? std::min(s->gate_rows, s->rows) : s->rows;
     p.groups = (s->rows + p.group_rows - 1) / p.group_rows;
-    p.slices = std::max<int64_t>(1, std::min(most / p.groups, (p.group_rows + teams - 1) / teams));
+    // as many slices of a group as let the workgroups, which are resident together, end together: the first multiple of a round
+    // whose last round is nine tenths full (65 532 rows of 512 in bf16, a gate for 100 rows each: forward and backward 168 us with
+    // one round at most, 160 us so)
+    const int64_t longest = (p.group_rows + teams - 1) / teams;
+    p.slices = 1;
+    for (int64_t rounds = 1; rounds <= 8; ++rounds) {
+        const int64_t cut = std::max<int64_t>(1, std::min(rounds * most / p.groups, longest)), units = p.groups * cut;
+        p.slices = cut;
+        if (cut == longest || 10 * units >= 9 * ((units + most - 1) / most * most)) break;
+    }
     p.unit_rows = (p.group_rows + p.slices - 1) / p.slices;
     p.unit_rows = (p.unit_rows + teams - 1) / teams * teams;
     p.slices = (p.group_rows + p.unit_rows - 1) / p.unit_rows;
@@ -418,7 +429,7 @@ template <typename T, int THREADS>
 int launch_fwd(const NormArgs& a, hipStream_t st) {
     using Team = RowTeam<THREADS>;
     // as many workgroups as are resident, of equal shares of the rows
-    const int64_t most = (int64_t)kNormBlocks * (sizeof(T) == 2 ? 5 : 4) * 256 / Team::kBlock;
+    const int64_t most = (int64_t)kNormCus * ((sizeof(T) == 2 ? 5 : 4) * 256 / Team::kBlock);
     const int64_t groups = (a.rows + Team::kRows - 1) / Team::kRows, each = (groups + most - 1) / most;
     const dim3 grid((unsigned)((groups + each - 1) / each));
     BPT_LAUNCH("residual_norm_kernel", (residual_norm_kernel<T, THREADS>), grid, dim3(Team::kBlock), 0, st, a);
@@ -434,6 +445,7 @@ int launch_bwd(const NormArgs& a, int blocks, hipStream_t st) {
 template <typename T>
 int launch_fwd_any(const NormArgs& a, hipStream_t st) {
     switch (norm_threads(a.d)) {
+        case 8: return launch_fwd<T, 8>(a, st);
         case 16: return launch_fwd<T, 16>(a, st);
         case 32: return launch_fwd<T, 32>(a, st);
         case 64: return launch_fwd<T, 64>(a, st);
@@ -445,6 +457,7 @@ int launch_fwd_any(const NormArgs& a, hipStream_t st) {
 template <typename T>
 int launch_bwd_any(const NormArgs& a, int blocks, hipStream_t st) {
     switch (norm_threads(a.d)) {
+        case 8: return launch_bwd<T, 8>(a, blocks, st);
         case 16: return launch_bwd<T, 16>(a, blocks, st);
         case 32: return launch_bwd<T, 32>(a, blocks, st);
         case 64: return launch_bwd<T, 64>(a, blocks, st);
