@@ -176,3 +176,35 @@ def test_results_are_the_same_twice_and_in_a_replayed_graph():
             torch.cuda.synchronize()
             assert all(torch.equal(want[k], got[k]) for k in want)
             assert torch.equal(bpt.bpt_gated_ffn_fwd(X, *W), want["Y"])
+
+
+@pytest.mark.parametrize("rows", [1, 16, 33])
+def test_few_rows_of_a_wide_block(rows):
+    # the hidden axis of the down product is cut for these: its parts are summed afterwards
+    X, dY, W = make(rows, 2048, 5464, rows)
+    check(both(X, dY, W, "silu", False), formulas(X, dY, W, "silu"))
+
+
+@pytest.mark.parametrize("rows,d,f,name", [(2000, 512, 1368, "silu"), (1858, 1344, 744, "gelu"), (3383, 1152, 432, "silu"), (4000, 512, 1368, "silu"),
+                                           (700, 1032, 2744, "gelu")])
+def test_gradients_of_middle_sizes(rows, d, f, name):
+    # dX and the weights' gradients share a launch, in tiles of different sizes
+    print("gated ffn", rows, d, f, name, flush=True)
+    X, dY, W = make(rows, d, f, rows + d + f)
+    check(both(X, dY, W, name, rows % 2 == 0), formulas(X, dY, W, name))
+
+
+@pytest.mark.parametrize("rows", [5, 300, 4000])
+def test_gradient_written_over_the_rows(rows):
+    import ctypes
+    X, dY, W = make(rows, 256, 520, 9)
+    want = formulas(X, dY, W, "silu")
+    dY, X = dY.contiguous(), X.contiguous()
+    s = bpt.BptGatedFfn(rows, 256, 520, bpt.BPT_BF16, 0, 256, bpt.BPT_F32)
+    L = bpt.load_library()
+    need = L.bpt_gated_ffn_bwd_workspace(ctypes.byref(s))
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    grads = [torch.empty(w.shape, device="cuda") for w in W]
+    assert L.bpt_gated_ffn_bwd(ctypes.byref(s), X.data_ptr(), *[w.data_ptr() for w in W], dY.data_ptr(), X.data_ptr(),
+                               *[g.data_ptr() for g in grads], ws.data_ptr(), need, int(torch.cuda.current_stream().cuda_stream)) == 0
+    check(dict(zip(("dX", "dWg", "dWu", "dWd"), [X] + grads)), want)

@@ -255,3 +255,11 @@ def test_results_are_the_same_twice_and_in_a_replayed_graph():
         torch.cuda.synchronize()
         assert all(torch.equal(want[k], got[k]) for k in want)
         assert all(torch.equal(want[k], v) for k, v in call(c, t).items())
+
+
+@pytest.mark.parametrize("rows,d,gate_rows", [(3000, 8, 0), (20011, 56, 7), (9001, 64, 100), (30000, 512, 100), (65532, 64, 2)])
+def test_narrow_rows_and_many_gates(rows, d, gate_rows):
+    print("residual norm", rows, d, gate_rows, flush=True)
+    for dtype in (torch.bfloat16, torch.float32):
+        c, t = make(rows, d, dtype, "rms", "layer", gate_rows, rows + d)
+        check(call(c, t), *formulas(c, t), dtype)
