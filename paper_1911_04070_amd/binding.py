@@ -778,17 +778,19 @@ def bpt_node_positions(g: Graph) -> torch.Tensor:
 
 def _row_stride(x: torch.Tensor, what: str) -> int:
     """Elements between the rows of a [..., d] tensor whose rows lie evenly apart."""
+    if x.is_contiguous():
+        return x.shape[-1]
     if x.stride(-1) != 1:
         raise ValueError("the features of %s must be contiguous" % what)
-    if x.dim() == 1:
-        return x.shape[0]
-    stride = x.stride(-2) if x.shape[-2] > 1 else max(x.stride(-2), x.shape[-1])
-    step = stride * x.shape[-2]
-    for i in range(x.dim() - 3, -1, -1):
-        if x.shape[i] > 1 and x.stride(i) != step:
+    stride = step = None
+    for i in range(x.dim() - 2, -1, -1):
+        if x.shape[i] == 1:      # (one index: its stride says nothing)
+            continue
+        if x.stride(i) != step and step is not None or x.stride(i) == 0:
             raise ValueError("the rows of %s must lie evenly apart" % what)
-        step *= x.shape[i]
-    return stride
+        stride = x.stride(i) if stride is None else stride
+        step = x.stride(i) * x.shape[i]
+    return x.shape[-1] if stride is None else stride
 
 
 def _same_strides(x: torch.Tensor) -> torch.Tensor:

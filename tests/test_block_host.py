@@ -165,3 +165,15 @@ def test_the_binding_takes_no_tensors_from_elsewhere():
         bpt.bpt_rotary(x.view(1, 1, 4, 64), None, torch.zeros(4))
     with pytest.raises(ValueError, match="cuda"):
         bpt.bpt_gated_ffn_fwd(x.bfloat16(), x, x, x)
+
+
+def test_rows_that_lie_evenly_apart():
+    base = torch.zeros((4, 6, 24))
+    for x, stride in ((base, 24), (base[:, :1], 144), (base[:, -1:], 144), (base[1:3, 2:3], 144), (base[..., :16], 24), (base[:1, ::2], 48),
+                      (base[0, 0], 24), (base[:1, :1], 24), (base[:0], 24), (base[:, :0], 24), (base.view(2, 2, 6, 24)[:, :, 5:], 144),
+                      (base.view(2, 2, 6, 24)[:, :1, 5:], 288)):
+        assert bpt._row_stride(x, "x") == stride, (x.shape, x.stride())
+    for x in (base[:, :3], base.transpose(0, 1), base.transpose(1, 2), base[..., ::2], base[:1].expand(4, 6, 24),
+              base[:, :1].expand(4, 6, 24), base[0, :1].expand(6, 24)):
+        with pytest.raises(ValueError):
+            bpt._row_stride(x, "x")
