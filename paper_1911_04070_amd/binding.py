@@ -12,6 +12,7 @@ from typing import Optional, Tuple
 
 import numpy as np
 import torch
+from torch.autograd.function import once_differentiable
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libbpt.so")
@@ -830,7 +831,8 @@ def bpt_residual_norm_fwd(x: torch.Tensor, branch: Optional[torch.Tensor], gate:
                           residual_scale: float = 1.0, eps: float = 1e-5, want_stats: bool = False):
     """y = residual_scale * x + gate * post(branch) and h = pre(y), post and pre "layer", "rms" or "none" (then h is None).
     x, branch: [..., d] in fp32 or bf16, equal layouts; gate: [ceil(rows / gate_rows), d] in their type, each row for gate_rows
-    consecutive rows; gains and biases fp32 [d] or None.  Returns (y, h), with want_stats (y, h, stats) for the backward."""
+    consecutive rows; gains and biases fp32 [d] or None.  Results lie as x does.
+    Returns (y, h), with want_stats (y, h, stats) for the backward."""
     s = _norm_args(x, branch, gate, post, pre, post_gain, post_bias, pre_gain, pre_bias, gate_rows, residual_scale, eps)
     y = _same_strides(x)
     h = _same_strides(x) if s.pre else None
@@ -925,10 +927,16 @@ def bpt_gated_ffn_bwd(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: t
 
 
 def _in_layout_of(x: torch.Tensor, g: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
-    """A gradient with the strides and dtype of x, which the calls ask for (autograd hands over any)."""
-    if g is None or (g.stride() == x.stride() and g.dtype == x.dtype):
+    """A gradient with the strides and dtype of x on a 16-byte boundary, as the calls ask for (autograd hands over any)."""
+    if g is None or (g.stride() == x.stride() and g.dtype == x.dtype and not g.data_ptr() & 15):
         return g
     return torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device).copy_(g)
+
+
+def _rows_usable(x: torch.Tensor) -> bool:
+    """Whether bpt_rotary takes x [B,H,N,D] as it lies (autograd hands over gradients in any layout)."""
+    s = x.stride()
+    return s[3] == 1 and not (s[0] | s[1] | s[2]) & 7 and not x.data_ptr() & 15
 
 
 class RotaryFunction(torch.autograd.Function):
@@ -942,11 +950,15 @@ class RotaryFunction(torch.autograd.Function):
         return bpt_rotary(Q, K, pos, **how)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dQ, dK):
         pos, = ctx.saved_tensors
+        dQ, dK = (g if g is None or _rows_usable(g) else g.clone(memory_format=torch.contiguous_format) for g in (dQ, dK))
         if dQ is not None and dK is not None:
-            return bpt_rotary(dQ.contiguous(), dK.contiguous(), pos, inverse=True, **ctx.how) + (None, None)
-        turned = [None if g is None else bpt_rotary(g.contiguous(), None, pos, inverse=True, **ctx.how)[0] for g in (dQ, dK)]
+            if dQ.stride() != dK.stride():
+                dQ, dK = dQ.contiguous(), dK.contiguous()   # (a copy lies on a boundary, what is contiguous already does too)
+            return bpt_rotary(dQ, dK, pos, inverse=True, **ctx.how) + (None, None)
+        turned = [None if g is None else bpt_rotary(g, None, pos, inverse=True, **ctx.how)[0] for g in (dQ, dK)]
         return (*turned, None, None)
 
 
@@ -970,6 +982,7 @@ class ResidualNormFunction(torch.autograd.Function):
         return y, h
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy, dh):
         x, branch, gate, stats, post_gain, post_bias, pre_gain, pre_bias = ctx.saved_tensors
         if dy is None and dh is None:
@@ -998,6 +1011,7 @@ class GatedFfnFunction(torch.autograd.Function):
         return bpt_gated_ffn_fwd(X, Wg, Wu, Wd, activation)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dY):
         X, Wg, Wu, Wd = ctx.saved_tensors
         return bpt_gated_ffn_bwd(X, Wg, Wu, Wd, _in_layout_of(X, dY), ctx.activation, bf16_grads=True) + (None,)

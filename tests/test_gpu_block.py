@@ -158,3 +158,14 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for i, v in enumerate(got):
         assert all(torch.equal(a, b) for a, b in zip(v, want[i % 2]))
+
+
+def test_gradients_off_the_boundary():
+    # autograd may hand over a gradient that starts anywhere
+    x = torch.randn((5, D), generator=torch.Generator().manual_seed(9)).bfloat16().cuda().requires_grad_()
+    p = parameters(10)
+    dy = torch.randn((5, D), generator=torch.Generator().manual_seed(11)).bfloat16().cuda()
+    off = torch.zeros(5 * D + 1, dtype=torch.bfloat16, device="cuda")[1:].view(5, D).copy_(dy)
+    for f in (lambda: bpt.residual_norm(x, x, pre="none")[0], lambda: bpt.residual_norm(x, x, pre="rms")[1],
+              lambda: bpt.gated_ffn(x, p["Wg"], p["Wu"], p["Wd"])):
+        assert torch.equal(*(torch.autograd.grad(f(), x, g)[0] for g in (dy, off)))

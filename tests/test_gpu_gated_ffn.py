@@ -208,3 +208,19 @@ def test_gradient_written_over_the_rows(rows):
     assert L.bpt_gated_ffn_bwd(ctypes.byref(s), X.data_ptr(), *[w.data_ptr() for w in W], dY.data_ptr(), X.data_ptr(),
                                *[g.data_ptr() for g in grads], ws.data_ptr(), need, int(torch.cuda.current_stream().cuda_stream)) == 0
     check(dict(zip(("dX", "dWg", "dWu", "dWd"), [X] + grads)), want)
+
+
+def test_rows_far_into_memory():
+    # rows and hidden rows whose elements lie more than 2^31 apart.  The partial sums over 2.2e6 rows of values of random sign stay
+    # below 2^-7 of the product of magnitudes, so that fp32 adds less than 2.2e6 * 2^-24 * 2^-7 / 8 of it (8 of 16 k to a rounding at
+    # least): 0.04 * 2^-8, within the docstring's 0.1
+    rows, d, f = 2200000, 64, 1032
+    X, dY, W = make(rows, d, f, 12, gap=960)
+    got = both(X, dY, W, "silu", False)
+    want = {}
+    for first in range(0, rows, 200000):
+        part = formulas(X[first:first + 200000], dY[first:first + 200000], W, "silu")
+        check({k: got[k][first:first + 200000] for k in ("Y", "dX")}, part)
+        for k in ("dWg", "dWu", "dWd"):
+            want[k] = part[k] if k not in want else tuple(a + b for a, b in zip(want[k], part[k]))
+    check({k: got[k] for k in want}, want)

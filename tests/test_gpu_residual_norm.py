@@ -263,3 +263,20 @@ def test_narrow_rows_and_many_gates(rows, d, gate_rows):
     for dtype in (torch.bfloat16, torch.float32):
         c, t = make(rows, d, dtype, "rms", "layer", gate_rows, rows + d)
         check(call(c, t), *formulas(c, t), dtype)
+
+
+def test_rows_far_into_memory():
+    # rows whose elements lie more than 2^31 apart
+    rows, d, stride = 1100000, 64, 2048
+    c, t = make(rows, d, torch.bfloat16, "rms", "layer", 1000, 11)
+    for k in ("x", "branch", "dy", "dh"):
+        t[k] = torch.empty((rows, stride), dtype=torch.bfloat16, device="cuda")[:, :d].copy_(t[k])
+    check(call(c, t), *formulas(c, t), torch.bfloat16)
+
+
+def test_second_derivatives_are_refused():
+    x = torch.randn((4, 64), device="cuda").requires_grad_()
+    y, h = bpt.residual_norm(x, x)
+    g, = torch.autograd.grad(h.square().sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(g.sum(), x)

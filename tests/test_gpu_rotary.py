@@ -155,3 +155,35 @@ def test_positions_of_the_nodes_of_a_packed_batch(lengths, shared):
     assert np.array_equal(got, want)
     g.destroy()
     tree.destroy()
+
+
+def test_rotary_gradients_of_any_layout():
+    # as autograd hands them over: rows of [B,N,H,64], different layouts for Q and K, gaps, one value for all
+    B, H, N = 2, 3, 37
+    pos = torch.arange(N, dtype=torch.float32, device="cuda")
+    for dtype in (torch.bfloat16, torch.float32):
+        for of_q, of_k in (("heads", "heads"), ("nodes", "nodes"), ("nodes", "heads"), ("gaps", "gaps")):
+            Q, K = (make(B, H, N, dtype, "nodes", s).requires_grad_() for s in (1, 2))
+            gq, gk = make(B, H, N, dtype, of_q, 3), make(B, H, N, dtype, of_k, 4)
+            got = torch.autograd.grad(bpt.rotary(Q, K, pos), (Q, K), (gq, gk))
+            for g, d in zip((gq, gk), got):
+                check(d, *reference(g, pos, 64, False, 10000.0, 1.0, 0, 1.0, 32.0, True), dtype)
+        Q = make(B, H, N, dtype, "heads", 1).requires_grad_()
+        for g in (torch.ones((), dtype=dtype, device="cuda").expand(Q.shape), make(1, 1, N, dtype, "heads", 5).expand(Q.shape),
+                  make(B, H, N + 1, dtype, "heads", 6).flatten()[4:4 + Q.numel()].view(Q.shape)):
+            d, = torch.autograd.grad(bpt.rotary(Q, None, pos)[0], Q, g)
+            check(d, *reference(g, pos, 64, False, 10000.0, 1.0, 0, 1.0, 32.0, True), dtype)
+
+
+def test_rotary_far_into_memory():
+    # rows whose elements lie more than 2^31 apart
+    N, H, wide = 1500000, 8, 1600
+    rows = torch.empty((1, N, wide), dtype=torch.bfloat16, device="cuda")
+    at = torch.tensor([0, 1, (1 << 31) // wide - 1, (1 << 31) // wide, (1 << 31) // wide + 1, N - 2, N - 1], device="cuda")
+    rows[:, at] = torch.randn((1, len(at), wide), generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    Q, K = (rows[:, :, 512 * i:512 * (i + 1)].view(1, N, H, 64).permute(0, 2, 1, 3) for i in range(2))
+    pos = torch.arange(N, dtype=torch.float32, device="cuda")
+    for out in (None, (Q, K)):
+        before = [x[:, :, at].clone() for x in (Q, K)]
+        for x, y in zip(before, bpt.bpt_rotary(Q, K, pos, out=out)):
+            check(y[:, :, at], *reference(x, pos[at], 64, False, 10000.0, 1.0, 0, 1.0, 32.0, False), torch.bfloat16)
