@@ -423,19 +423,23 @@ constexpr int kCus = 256;
 
 // Sizes of a workgroup's tile.  kBig: 256 x 256, slabs of 64, one workgroup of 8 wavefronts per compute unit; kWide: 128 x 256,
 // slabs of 32, three deep, and kMid: 128 x 128, slabs of 64: two workgroups of 4 wavefronts per compute unit, of which
-// one multiplies while the other starts up or writes; kSmall: 64 x 64, slabs of 64, four deep: for products of few tiles, whose
-// time is the slabs' latency.  Times measured on all four products of the block (both operands' orders differ by 10 %).
-enum TileSize { kBig, kWide, kMid, kSmall };
+// one multiplies while the other starts up or writes; kSmall and kSmallAcross: 64 x 64, slabs of 128, two deep, or of 64, four deep,
+// where A lies across k (the weights' gradients, whose sums over rows are short): for products of few tiles, whose
+// time is a slab's start, four dependent matrix instructions and its barrier (forward and backward of 700 rows, d = 1024,
+// f = 2736: 108 us with slabs of 64 throughout, 98 us so; 400 rows, d = 2048, f = 5464, slabs of 128 throughout: 192 -> 216 us; a
+// fifth slab in flight changes nothing).  Times measured on all four products of the block (both operands' orders differ by 10 %).
+enum TileSize { kBig, kWide, kMid, kSmall, kSmallAcross };
 struct TileCost {
     int m, n, slab, per_cu;
     float us, us_one, us_few;   // of 64 k: the device full; one workgroup on every compute unit; few compute units busy
 };
 constexpr TileCost kTileCost[] = {{256, 256, 64, 1, 2.1f, 2.1f, 1.45f}, {128, 256, 32, 2, 2.35f, 1.7f, 1.15f}, {128, 128, 64, 2, 1.25f, 0.92f, 0.60f},
-                                  {64, 64, 64, 2, 0.53f, 0.43f, 0.37f}};
+                                  {64, 64, 128, 2, 0.53f, 0.43f, 0.35f}, {64, 64, 64, 2, 0.53f, 0.43f, 0.37f}};
 float slab_us(const TileCost& t, int64_t groups) {   // in between, in proportion
     if (groups <= kCus) return t.us_few + (t.us_one - t.us_few) * (float)groups / kCus;
     return t.us_one + (t.us - t.us_one) * std::min(1.f, (float)(groups - kCus) / kCus);
 }
+constexpr float kGapUs = 1.0f;               // between two launches
 constexpr float kStartUs = 2.5f;             // a tile's first loads and its results
 constexpr float kSumUs = 3.5f, kSumBytesPerUs = 5.0e6f;   // adding up slices: a launch, and their bytes written and read
 constexpr int kMaxSlices = 32, kMinSliceK = 128;
@@ -447,13 +451,13 @@ struct ProductPlan {
 };
 // The cheapest of the tile sizes and slicings by the costs above: whole tiles run in rounds of what the device holds; the last
 // round's, if they leave much of it idle, are cut along k instead.
-ProductPlan plan_product(int64_t M, int64_t N, int64_t K, int terms, int matrices) {
+ProductPlan plan_product(int64_t M, int64_t N, int64_t K, int terms, int matrices, TileSize small) {
     ProductPlan best = {};
     best.us = INFINITY;
-    for (int c = kBig; c <= kSmall; ++c) {
+    for (TileSize c : {kBig, kWide, kMid, small}) {
         const TileCost& t = kTileCost[c];
         ProductPlan p = {};
-        p.size = (TileSize)c;
+        p.size = c;
         p.tiles_m = (int)((M + t.m - 1) / t.m);
         p.tiles_n = (int)((N + t.n - 1) / t.n);
         const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * matrices, slots = (int64_t)kCus * t.per_cu;
@@ -500,7 +504,7 @@ int launch_product(ProductArgs& g, const ProductPlan& p, void* part, hipStream_t
     if (p.size == kBig) return launch_product<Tile<256, 256, 2, 4, 64, 2, AK, BK, false>, AK, BK, T>(g, p.left, st);
     if (p.size == kWide) return launch_product<Tile<128, 256, 1, 4, 32, 3, AK, BK, false>, AK, BK, T>(g, p.left, st);
     if (p.size == kMid) return launch_product<Tile<128, 128, 2, 2, 64, 2, AK, BK, false>, AK, BK, T>(g, p.left, st);
-    return launch_product<Tile<64, 64, 2, 2, 64, 4, AK, BK, false>, AK, BK, T>(g, p.left, st);
+    return launch_product<Tile<64, 64, 2, 2, AK ? 128 : 64, AK ? 2 : 4, AK, BK, false>, AK, BK, T>(g, p.left, st);
 }
 
 // Strips of 32 x 32 serve as long as every one has a compute unit to itself (d = 512, f = 1368: 1 row, both products 6.7 + 9.9
@@ -543,7 +547,7 @@ int launch_up(UpArgs& g, hipStream_t st) {
     const HiddenSize size = hidden_tiles(g.M, g.f, false, g.tiles_m, g.tiles_n);
     if (size == kHiddenWide) return launch_up_as<ACT, Tile<128, 256, 2, 2, 32, 3, true, false, true>>(g, st);
     if (size == kHiddenMid) return launch_up_as<ACT, Tile<128, 128, 2, 2, 64, 2, true, false, true>>(g, st);
-    return launch_up_as<ACT, Tile<64, 128, 2, 2, 64, 4, true, false, true>>(g, st);
+    return launch_up_as<ACT, Tile<64, 128, 2, 2, 128, 2, true, false, true>>(g, st);
 }
 
 template <int ACT, typename C, typename C2>
@@ -562,7 +566,7 @@ int launch_hidden(HiddenArgs& g, hipStream_t st) {
         return launch_hidden_as<ACT, Tile<128, 256, 1, 4, 32, 3, true, false, true>, Tile<128, 128, 1, 4, 32, 3, true, true, false>>(g, st);
     if (size == kHiddenMid)
         return launch_hidden_as<ACT, Tile<128, 128, 2, 2, 64, 2, true, false, true>, Tile<128, 64, 2, 2, 64, 2, true, true, false>>(g, st);
-    return launch_hidden_as<ACT, Tile<64, 128, 2, 2, 64, 4, true, false, true>, Tile<64, 64, 2, 2, 64, 4, true, true, false>>(g, st);
+    return launch_hidden_as<ACT, Tile<64, 128, 2, 2, 128, 2, true, false, true>, Tile<64, 64, 2, 2, 128, 2, true, true, false>>(g, st);
 }
 
 int check_ffn(const bpt_gated_ffn_t* s) {
@@ -595,7 +599,7 @@ FwdBuffers fwd_buffers(const bpt_gated_ffn_t* s) {
     FwdBuffers b = {};
     b.up_strips = use_strips(s->rows, s->f);
     b.down_strips = use_strips(s->rows, s->d);
-    if (!b.down_strips) b.down = plan_product(s->rows, s->d, s->f, 1, 1);
+    if (!b.down_strips) b.down = plan_product(s->rows, s->d, s->f, 1, 1, kSmall);
     const size_t hidden = align256((size_t)s->rows * s->f * 2);
     b.F = 0;
     b.F_low = hidden;
@@ -615,9 +619,9 @@ struct BwdBuffers {
 };
 BwdBuffers bwd_buffers(const bpt_gated_ffn_t* s) {
     BwdBuffers b = {};
-    b.wd = plan_product(s->f, s->d, s->rows, 1, 1);
-    b.wgu = plan_product(s->d, s->f, s->rows, 1, 2);
-    b.dx = plan_product(s->rows, s->d, s->f, 2, 1);
+    b.wd = plan_product(s->f, s->d, s->rows, 1, 1, kSmallAcross);
+    b.wgu = plan_product(s->d, s->f, s->rows, 1, 2, kSmallAcross);
+    b.dx = plan_product(s->rows, s->d, s->f, 2, 1, kSmall);
     const size_t hidden = align256((size_t)s->rows * s->f * 2);
     b.F = 0;
     b.dG = hidden;
@@ -672,14 +676,15 @@ float plan_together(GradArgs& g, TileSize x, TileSize w) {
     }
     float longest = 0.f, work = 0.f;
     for (int i = 0; i < 3; ++i) {
-        const float us = (float)slabs[i] * slab_us(kTileCost[i == 0 ? x : w], groups);
+        const TileCost& t = kTileCost[i == 0 ? x : w];
+        const float us = (float)slabs[i] * t.slab / 64 * slab_us(t, groups);
         longest = std::max(longest, us);
         work += (float)product[i]->full * us;
     }
-    g.dx_last = slabs[0] < slabs[1];
+    g.dx_last = slabs[0] * kTileCost[x].slab < slabs[1] * kTileCost[w].slab;
     if (groups <= 2 * kCus) return kStartUs + longest;   // (two of either size per compute unit)
-    // several rounds of unequal lengths: measured up to a quarter over their mean
-    return kStartUs + 1.25f * std::max(longest, work / (2 * kCus));
+    // several rounds of unequal lengths: measured up to 28 % over their mean
+    return kStartUs + std::max(longest, 1.28f * work / (2 * kCus));
 }
 
 template <typename CX, typename CW, typename T>
@@ -693,10 +698,10 @@ template <typename T>
 int grads(const bpt_gated_ffn_t* s, const BwdBuffers& b, GradArgs& g, bool dx_alone, void* part, hipStream_t st) {
     if (s->rows > 0 && !dx_alone) {
         GradArgs best = g;
-        float us = b.dx.us + b.wgu.us + b.wd.us;
+        float us = b.dx.us + b.wgu.us + b.wd.us + 2 * kGapUs;
         TileSize size[2] = {kBig, kBig};
         for (TileSize x : {kMid, kSmall})
-            for (TileSize w : {kMid, kSmall}) {
+            for (TileSize w : {kMid, kSmallAcross}) {
                 GradArgs a = g;
                 const float t = plan_together(a, x, w);
                 if (t >= us) continue;
@@ -707,7 +712,7 @@ int grads(const bpt_gated_ffn_t* s, const BwdBuffers& b, GradArgs& g, bool dx_al
             }
         using MidX = Tile<128, 128, 2, 2, 64, 2, true, true, false>;
         using MidW = Tile<128, 128, 2, 2, 64, 2, false, false, false>;
-        using SmallX = Tile<64, 64, 2, 2, 64, 4, true, true, false>;
+        using SmallX = Tile<64, 64, 2, 2, 128, 2, true, true, false>;
         using SmallW = Tile<64, 64, 2, 2, 64, 4, false, false, false>;
         if (size[0] == kMid) return size[1] == kMid ? launch_grads<MidX, MidW, T>(best, st) : launch_grads<MidX, SmallW, T>(best, st);
         if (size[0] == kSmall) return size[1] == kMid ? launch_grads<SmallX, MidW, T>(best, st) : launch_grads<SmallX, SmallW, T>(best, st);

@@ -1,6 +1,6 @@
 // Tiles of a matrix product C[m][n] = sum_k A[m][k] B[k][n] on the matrix cores, for the feed-forward block: bf16 operands,
-// fp32 sums.  A workgroup computes BM x BN of C in WR x WC wavefronts; both operands go through LDS in slabs of 32 or 64 k,
-// two or three slabs deep, loaded straight into LDS (no registers in between).
+// fp32 sums.  A workgroup computes BM x BN of C in WR x WC wavefronts; both operands go through LDS in slabs of 32 to 128 k,
+// two to four slabs deep, loaded straight into LDS (no registers in between).
 //
 // An operand lies in memory with either k or its own index (m or n) contiguous, and is kept that way in LDS:
 //   k contiguous     [W][SLAB]  read 16 bytes per lane (8 k of one row)
@@ -60,7 +60,7 @@ __device__ __forceinline__ int piece_swap(int k) {
 // different pieces of 256 bytes (the banks' width)
 template <int SLAB>
 __device__ __forceinline__ int row_swap(int row) {
-    return SLAB == 64 ? ((row >> 1) & 7) : ((row >> 2) & 3);
+    return SLAB == 128 ? (row & 15) : SLAB == 64 ? ((row >> 1) & 7) : ((row >> 2) & 3);
 }
 
 // Loads a slab of an operand of W rows (or columns) into LDS with WAVES wavefronts.
