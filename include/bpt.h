@@ -408,7 +408,8 @@ int bpt_stack_bwd(const bpt_graph_t* g, int32_t B, int32_t H, int32_t num_layers
 typedef struct {
     int32_t B, H, N, D;   /* batch, heads, rows (any count, also 0), head width (D must be 64) */
     int32_t dtype;        /* bpt_dtype_t of Q, K and the results */
-    int64_t stride_b, stride_h, stride_n;             /* of Q and K, in elements; multiples of 8, not negative */
+    int64_t stride_b, stride_h, stride_n;             /* of Q and K, in elements; multiples of 8, not negative (here and
+                                                         below: where B, H or N is 1, its strides are not looked at) */
     int64_t out_stride_b, out_stride_h, out_stride_n; /* of Qr and Kr; multiples of 8; no two rows may overlap: in the
                                                          order of their size, each is at least the one before times its
                                                          count (the smallest at least D) */

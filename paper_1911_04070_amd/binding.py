@@ -735,6 +735,16 @@ def _rotary_out(x: torch.Tensor) -> torch.Tensor:
     return torch.empty((B, H, N, D), dtype=x.dtype, device=x.device)
 
 
+def _head_strides(x: torch.Tensor) -> Tuple[int, ...]:
+    """Strides of [B,H,N,D], 0 for an axis of one entry: torch sets those to anything."""
+    return tuple(0 if n == 1 else s for n, s in zip(x.shape, x.stride()))
+
+
+def _lie_alike(x: torch.Tensor, y: torch.Tensor) -> bool:
+    """Whether the heads and rows of two [B,H,N,D] tensors of one shape lie equally far apart."""
+    return x.stride() == y.stride() or _head_strides(x) == _head_strides(y)
+
+
 def bpt_rotary(Q: torch.Tensor, K: Optional[torch.Tensor], pos: torch.Tensor, rot: Optional[int] = None, interleaved: bool = False,
                base: float = 10000.0, factor: float = 1.0, context: float = 0, low: float = 1.0, high: float = 32.0,
                inverse: bool = False, out=None):
@@ -748,7 +758,7 @@ def bpt_rotary(Q: torch.Tensor, K: Optional[torch.Tensor], pos: torch.Tensor, ro
     dt = _DTYPES.get(Q.dtype)
     if dt is None:
         raise ValueError("dtype must be float32 or bfloat16")
-    if K is not None and (K.dtype != Q.dtype or K.shape != Q.shape or K.stride() != Q.stride() or K.device != dev):
+    if K is not None and (K.dtype != Q.dtype or K.shape != Q.shape or not _lie_alike(K, Q) or K.device != dev):
         raise ValueError("Q and K must share dtype, shape, strides and device")
     B, H, N, D = Q.shape
     if pos.dtype != torch.float32 or pos.device != dev or tuple(pos.shape) not in ((N,), (B, N)) or (N > 1 and pos.stride(-1) != 1):
@@ -760,7 +770,7 @@ def bpt_rotary(Q: torch.Tensor, K: Optional[torch.Tensor], pos: torch.Tensor, ro
         if (Kr is None) != (K is None):
             raise ValueError("out must hold a tensor for each of Q and K")
         for t in (Qr,) if Kr is None else (Qr, Kr):
-            if t.dtype != Q.dtype or t.shape != Q.shape or t.stride() != Qr.stride() or t.stride(3) != 1 or t.device != dev:
+            if t.dtype != Q.dtype or t.shape != Q.shape or not _lie_alike(t, Qr) or t.stride(3) != 1 or t.device != dev:
                 raise ValueError("the results must have Q's dtype, shape and device and share strides")
     s, o = Q.stride(), Qr.stride()
     shp = BptRotary(B, H, N, D, dt, s[0], s[1], s[2], o[0], o[1], o[2], D if rot is None else int(rot), bool(interleaved), bool(inverse),
@@ -935,8 +945,8 @@ def _in_layout_of(x: torch.Tensor, g: Optional[torch.Tensor]) -> Optional[torch.
 
 def _rows_usable(x: torch.Tensor) -> bool:
     """Whether bpt_rotary takes x [B,H,N,D] as it lies (autograd hands over gradients in any layout)."""
-    s = x.stride()
-    return s[3] == 1 and not (s[0] | s[1] | s[2]) & 7 and not x.data_ptr() & 15
+    b, h, n, _ = _head_strides(x)
+    return x.stride(3) == 1 and not (b | h | n) & 7 and not x.data_ptr() & 15
 
 
 class RotaryFunction(torch.autograd.Function):
@@ -954,10 +964,9 @@ class RotaryFunction(torch.autograd.Function):
     def backward(ctx, dQ, dK):
         pos, = ctx.saved_tensors
         dQ, dK = (g if g is None or _rows_usable(g) else g.clone(memory_format=torch.contiguous_format) for g in (dQ, dK))
-        if dQ is not None and dK is not None:
-            if dQ.stride() != dK.stride():
-                dQ, dK = dQ.contiguous(), dK.contiguous()   # (a copy lies on a boundary, what is contiguous already does too)
+        if dQ is not None and dK is not None and _lie_alike(dQ, dK):
             return bpt_rotary(dQ, dK, pos, inverse=True, **ctx.how) + (None, None)
+        # (one is missing, or they lie in different orders: each in a call of its own, as it lies)
         turned = [None if g is None else bpt_rotary(g, None, pos, inverse=True, **ctx.how)[0] for g in (dQ, dK)]
         return (*turned, None, None)
 

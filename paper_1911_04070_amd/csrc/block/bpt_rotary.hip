@@ -212,9 +212,12 @@ int bpt_rotary(const bpt_rotary_t* s, const float* pos, int64_t pos_stride_b, co
     if (!s || s->B < 0 || s->H < 0 || s->N < 0) return BPT_ERR_INVALID_ARG;
     if (s->D != kD || (s->dtype != BPT_F32 && s->dtype != BPT_BF16)) return BPT_ERR_UNSUPPORTED;
     if (s->rot < 2 || s->rot > kD || (s->rot & 1)) return BPT_ERR_INVALID_ARG;
-    const int64_t in[3] = {s->stride_b, s->stride_h, s->stride_n}, out[3] = {s->out_stride_b, s->out_stride_h, s->out_stride_n};
-    for (int i = 0; i < 3; ++i)
+    int64_t in[3] = {s->stride_b, s->stride_h, s->stride_n}, out[3] = {s->out_stride_b, s->out_stride_h, s->out_stride_n};
+    const int32_t count[3] = {s->B, s->H, s->N};
+    for (int i = 0; i < 3; ++i) {
+        if (count[i] == 1) in[i] = out[i] = 0;   // (one entry: its stride says nothing)
         if (in[i] < 0 || out[i] < 0 || ((in[i] | out[i]) & 7)) return BPT_ERR_INVALID_ARG;
+    }
     const double base = s->base > 0 ? s->base : 10000.0, factor = s->factor > 0 ? s->factor : 1.0;
     const double low = s->low == 0 && s->high == 0 ? 1.0 : s->low, high = s->low == 0 && s->high == 0 ? 32.0 : s->high;
     if (!(std::isfinite(base) && std::isfinite(factor) && std::isfinite(s->context) && s->context >= 0 && low < high) ||
@@ -225,7 +228,7 @@ int bpt_rotary(const bpt_rotary_t* s, const float* pos, int64_t pos_stride_b, co
     if (rows == 0 || s->H == 0) return BPT_OK;
     if (!pos || !Q || !Qr || !K != !Kr || (reinterpret_cast<uintptr_t>(pos) & 3) || off_boundary(Q, K, Qr, Kr) || Qr == Kr) return BPT_ERR_INVALID_ARG;
     if (!rows_apart(s->B, s->H, s->N, out[0], out[1], out[2])) return BPT_ERR_INVALID_ARG;
-    const bool same = (s->B == 1 || in[0] == out[0]) && (s->H == 1 || in[1] == out[1]) && (s->N == 1 || in[2] == out[2]);
+    const bool same = in[0] == out[0] && in[1] == out[1] && in[2] == out[2];
     if (((Q == Qr || (K && K == Kr)) && !same) || Qr == K || (Kr && Kr == Q)) return BPT_ERR_INVALID_ARG;
     RotaryArgs a = {};
     a.in[0] = Q; a.in[1] = K;
@@ -235,7 +238,7 @@ int bpt_rotary(const bpt_rotary_t* s, const float* pos, int64_t pos_stride_b, co
     a.ob = out[0]; a.oh = out[1]; a.on = out[2];
     a.N = s->N; a.H = s->H; a.rot = s->rot;
     a.rows = rows;
-    a.heads_first = in[1] < in[2];
+    a.heads_first = in[1] < (s->N == 1 ? in[0] : in[2]);
     const double kTwoPi = 6.283185307179586476925286766559;
     const double step = std::pow(base, -2.0 / s->rot);
     double w = 1.0;   // 32 products of the step at most: relative error below 32 * 2^-53
