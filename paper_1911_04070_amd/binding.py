@@ -809,8 +809,9 @@ def _same_strides(x: torch.Tensor) -> torch.Tensor:
 
 
 def _like(x: torch.Tensor, t: torch.Tensor, what: str) -> None:
-    if t.dtype != x.dtype or t.shape != x.shape or t.stride() != x.stride() or t.device != x.device:
-        raise ValueError("%s must have the dtype, shape, strides and device of x" % what)
+    if t.dtype != x.dtype or t.shape != x.shape or t.device != x.device or (
+            t.stride() != x.stride() and _row_stride(t, what) != _row_stride(x, "x")):   # (axes of one entry may have any stride)
+        raise ValueError("%s must have the dtype, shape, distance of rows and device of x" % what)
 
 
 def _norm_args(x, branch, gate, post, pre, post_gain, post_bias, pre_gain, pre_bias, gate_rows, residual_scale, eps):

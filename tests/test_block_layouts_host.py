@@ -108,3 +108,31 @@ def test_the_library_does_not_look_at_strides_of_unit_axes():
         # no heads or no rows: nothing to do, and nothing refused
         other = "H" if count != "H" else "N"
         assert call(**{count: 1, other: 0}, **odd) == bpt.BPT_OK
+
+
+def one_layout(rows=6, d=64, dtype=torch.bfloat16):
+    """[1, rows, d] tensors that lie alike, with different strides of the axis of one entry"""
+    x = torch.zeros((1, rows, d), dtype=dtype)
+    return [x, torch.zeros((rows, 1, d), dtype=dtype).transpose(0, 1), x.as_strided(x.shape, (7, d, 1))]
+
+
+def test_rows_with_unit_axes(recorder):
+    d = 64
+    W = [torch.zeros((d, 128), dtype=torch.bfloat16), torch.zeros((d, 128), dtype=torch.bfloat16), torch.zeros((128, d), dtype=torch.bfloat16)]
+    stats = torch.zeros((6, 4))
+    for a in one_layout():
+        for b in one_layout():
+            y, h = bpt.bpt_residual_norm_fwd(a, b)
+            assert y.shape == h.shape == a.shape
+            got = bpt.bpt_residual_norm_bwd(a, b, None, stats, b, a)
+            assert got["dx"].shape == got["d_branch"].shape == a.shape
+            assert bpt.bpt_gated_ffn_fwd(a, *W, out=b) is b
+            assert bpt.bpt_gated_ffn_bwd(a, *W, b)[0].shape == a.shape
+
+
+def test_rows_that_differ_are_refused(recorder):
+    x = torch.zeros((1, 6, 64), dtype=torch.bfloat16)
+    for other in (x[:, :5], x.float(), torch.zeros((6, 1, 64), dtype=torch.bfloat16), torch.zeros((1, 6, 128), dtype=torch.bfloat16)[..., ::2],
+                  x[:, :1].expand(1, 6, 64)):
+        with pytest.raises(ValueError):
+            bpt.bpt_residual_norm_fwd(x, other)

@@ -24,3 +24,24 @@ def test_rotary_with_unit_axes(shape, dtype):
         gq, gk = make_heads(B, H, N, dtype, of_q, 3), make_heads(B, H, N, dtype, of_k, 4)
         for g, d in zip((gq, gk), torch.autograd.grad(bpt.rotary(Q, K, pos), (Q, K), (gq, gk))):
             check_rotary(d, *turned(g, pos, 64, False, 10000.0, 1.0, 0, 1.0, 32.0, True), dtype)
+
+
+def test_rows_with_unit_axes():
+    # [1, rows, d] against [rows, 1, d] turned round: the same rows in the same places
+    gen = torch.Generator().manual_seed(1)
+    r = lambda *s: torch.randn(s, generator=gen).bfloat16().cuda()
+    rows, d, f = 37, 64, 136
+    W = [r(d, f) * 0.125, r(d, f) * 0.125, r(f, d) * 0.0625]
+    x, b, dy = r(rows, d), r(rows, d), r(rows, d)
+    dense = lambda t: t.view(1, rows, d)
+    turned_round = lambda t: t.view(rows, 1, d).transpose(0, 1)
+
+    def work(place, other):
+        X, B = place(x).requires_grad_(), other(b).requires_grad_()
+        y, h = bpt.residual_norm(X, B)
+        Y = bpt.gated_ffn(X, *W)
+        return (y, h, Y) + torch.autograd.grad((y, h, Y), (X, B), (other(dy), place(dy), other(dy)))
+
+    want = work(dense, dense)
+    for place, other in ((dense, turned_round), (turned_round, dense), (turned_round, turned_round)):
+        assert all(torch.equal(a, w) for a, w in zip(work(place, other), want))
