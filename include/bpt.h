@@ -435,6 +435,15 @@ int bpt_rotary(const bpt_rotary_t* s, const float* pos, int64_t pos_stride_b, co
  * padded tree).  pos: device, num_nodes fp32. */
 int bpt_node_positions(const bpt_graph_t* g, float* pos, void* stream);
 
+/* Elements between the rows of a call's tensors where these do not all lie alike (a slice of a larger tensor beside a dense one):
+ * each at least d and a multiple of 8.  Calls that take these do not use the `stride` of their shape (which has to be valid). */
+typedef struct {
+    int64_t x;       /* x; X */
+    int64_t branch;  /* branch (bpt_residual_norm_*) */
+    int64_t out;     /* what the call writes: y and h, dx and d_branch; Y, dX */
+    int64_t grad;    /* what a backward is given: dy and dh; dY */
+} bpt_row_strides_t;
+
 typedef enum { BPT_NORM_NONE = 0, BPT_NORM_LAYER = 1, BPT_NORM_RMS = 2 } bpt_norm_t;
 
 /* Norms before and after a sublayer with its gate and the residual sum, for every row:
@@ -458,10 +467,14 @@ typedef struct {
 /* branch may be NULL with post = NONE and gate_rows = 0 (y = residual_scale * x: the norm before the first sublayer).
  * Gains and biases: fp32 [d], NULL for 1 and 0 (and NULL where the norm is NONE).  y may be NULL where it is not
  * wanted, h is NULL exactly where pre = NONE.  stats: fp32 [rows][4] (of branch and of y: mean, 1 / deviation) for the
- * backward, or NULL.  y may be x or branch itself, and h too where it is not y; other overlaps are not allowed. */
+ * backward, or NULL.  y may be x or branch itself, and h too where it is not y (with equal strides); other overlaps are not
+ * allowed.  The second call is the same with strides of their own for the tensors; strides = NULL: s->stride for all. */
 int bpt_residual_norm_fwd(const bpt_residual_norm_t* s, const void* x, const void* branch, const void* gate,
                           const float* post_gain, const float* post_bias, const float* pre_gain, const float* pre_bias,
                           void* y, void* h, float* stats, void* stream);
+int bpt_residual_norm_fwd_strided(const bpt_residual_norm_t* s, const bpt_row_strides_t* strides, const void* x, const void* branch,
+                                  const void* gate, const float* post_gain, const float* post_bias, const float* pre_gain,
+                                  const float* pre_bias, void* y, void* h, float* stats, void* stream);
 
 /* Gradients of bpt_residual_norm_fwd, fp32 [d] (d_gate: the tensors' type, the gate's shape); each is NULL exactly
  * where its parameter is. */
@@ -472,14 +485,18 @@ typedef struct {
 
 /* Backward: given the gradients dy and dh of a scalar with respect to y and h (either may be NULL and counts as zero;
  * dh is NULL where pre = NONE), writes dx, d_branch (NULL exactly where branch is) and the parameters' gradients.  x,
- * branch, gate, gains, post_bias and stats as the forward had and left them.  dx and d_branch may be dy or dh themselves;
- * other overlaps are not allowed.  Column sums are formed in a fixed order: results are run-to-run identical.
+ * branch, gate, gains, post_bias and stats as the forward had and left them.  dx and d_branch may be dy or dh themselves (with
+ * equal strides); other overlaps are not allowed.  The last call is the same with strides of their own for the tensors.  Column sums are formed in a fixed order: results are run-to-run identical.
  * workspace: at least bpt_residual_norm_bwd_workspace bytes (SIZE_MAX for a shape that the calls refuse). */
 size_t bpt_residual_norm_bwd_workspace(const bpt_residual_norm_t* s);
 int bpt_residual_norm_bwd(const bpt_residual_norm_t* s, const void* x, const void* branch, const void* gate,
                           const float* post_gain, const float* post_bias, const float* pre_gain, const float* pre_bias,
                           const float* stats, const void* dy, const void* dh, void* dx, void* d_branch,
                           const bpt_residual_norm_grads_t* grads, void* workspace, size_t workspace_bytes, void* stream);
+int bpt_residual_norm_bwd_strided(const bpt_residual_norm_t* s, const bpt_row_strides_t* strides, const void* x, const void* branch,
+                                  const void* gate, const float* post_gain, const float* post_bias, const float* pre_gain,
+                                  const float* pre_bias, const float* stats, const void* dy, const void* dh, void* dx, void* d_branch,
+                                  const bpt_residual_norm_grads_t* grads, void* workspace, size_t workspace_bytes, void* stream);
 
 typedef enum { BPT_ACT_SILU = 0, BPT_ACT_GELU = 1, BPT_ACT_RELU = 2 } bpt_activation_t;
 
@@ -498,19 +515,26 @@ typedef struct {
 } bpt_gated_ffn_t;
 
 /* workspace: at least bpt_gated_ffn_fwd_workspace bytes (SIZE_MAX for a shape that the calls refuse); its contents are not
- * needed by the backward.  Y must not overlap X. */
+ * needed by the backward.  Y must not overlap X.  The last call is the same with strides of their own for the tensors, each < 2^20;
+ * strides = NULL: s->stride for all. */
 size_t bpt_gated_ffn_fwd_workspace(const bpt_gated_ffn_t* s);
 int bpt_gated_ffn_fwd(const bpt_gated_ffn_t* s, const void* X, const void* Wg, const void* Wu, const void* Wd, void* Y,
                       void* workspace, size_t workspace_bytes, void* stream);
+int bpt_gated_ffn_fwd_strided(const bpt_gated_ffn_t* s, const bpt_row_strides_t* strides, const void* X, const void* Wg, const void* Wu,
+                              const void* Wd, void* Y, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Backward: with G = X Wg, U = X Wu formed again (nothing is kept between the calls),  dF = dY Wd^T,
  * dG = dF * U * act'(G), dU = dF * act(G),  writes  dX = dG Wg^T + dU Wu^T,  dWg = X^T dG, dWu = X^T dU and
  * dWd = (act(G) * U)^T dY (contiguous, grad_dtype).  act'(0) = 0 for RELU.  Sums over rows are cut into slices that are
- * added in a fixed order; results are run-to-run identical.  dX may be dY itself, or X; other overlaps are not allowed. */
+ * added in a fixed order; results are run-to-run identical.  dX may be dY itself, or X (with equal strides); other overlaps are
+ * not allowed.  The last call is the same with strides of their own for the tensors. */
 size_t bpt_gated_ffn_bwd_workspace(const bpt_gated_ffn_t* s);
 int bpt_gated_ffn_bwd(const bpt_gated_ffn_t* s, const void* X, const void* Wg, const void* Wu, const void* Wd,
                       const void* dY, void* dX, void* dWg, void* dWu, void* dWd, void* workspace, size_t workspace_bytes,
                       void* stream);
+int bpt_gated_ffn_bwd_strided(const bpt_gated_ffn_t* s, const bpt_row_strides_t* strides, const void* X, const void* Wg, const void* Wu,
+                              const void* Wd, const void* dY, void* dX, void* dWg, void* dWu, void* dWd, void* workspace,
+                              size_t workspace_bytes, void* stream);
 
 /* Sec. 3.2 with the rule for shorter sequences stated at the top of this header: the number
  * of edges of the graph over n tokens with density k that a sequence of len tokens keeps

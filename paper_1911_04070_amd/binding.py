@@ -29,6 +29,7 @@ EXPORTS = [
     "bpt_stack_fwd_workspace", "bpt_stack_fwd", "bpt_stack_bwd_workspace", "bpt_stack_bwd",
     "bpt_count_edges", "bpt_strerror", "bpt_rotary", "bpt_node_positions", "bpt_residual_norm_fwd", "bpt_residual_norm_bwd_workspace",
     "bpt_residual_norm_bwd", "bpt_gated_ffn_fwd_workspace", "bpt_gated_ffn_fwd", "bpt_gated_ffn_bwd_workspace", "bpt_gated_ffn_bwd",
+    "bpt_residual_norm_fwd_strided", "bpt_residual_norm_bwd_strided", "bpt_gated_ffn_fwd_strided", "bpt_gated_ffn_bwd_strided",
 ]
 
 
@@ -62,6 +63,10 @@ class BptResidualNorm(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("d", ctypes.c_int32), ("dtype", ctypes.c_int32), ("stride", ctypes.c_int64),
                 ("post", ctypes.c_int32), ("pre", ctypes.c_int32), ("gate_rows", ctypes.c_int64),
                 ("residual_scale", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+class BptRowStrides(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("x", "branch", "out", "grad")]
 
 
 class BptResidualNormGrads(ctypes.Structure):
@@ -172,6 +177,10 @@ def load_library() -> ctypes.CDLL:
     L.bpt_gated_ffn_bwd_workspace.argtypes = [P(BptGatedFfn)]
     L.bpt_gated_ffn_bwd.restype = ctypes.c_int
     L.bpt_gated_ffn_bwd.argtypes = [P(BptGatedFfn)] + [vp] * 10 + [sz, vp]
+    for name in ("bpt_residual_norm_fwd", "bpt_residual_norm_bwd", "bpt_gated_ffn_fwd", "bpt_gated_ffn_bwd"):
+        plain, strided = getattr(L, name), getattr(L, name + "_strided")
+        strided.restype = ctypes.c_int
+        strided.argtypes = plain.argtypes[:1] + [P(BptRowStrides)] + plain.argtypes[1:]
     L.bpt_strerror.restype = ctypes.c_char_p
     L.bpt_strerror.argtypes = [ctypes.c_int]
     _lib = L
@@ -804,14 +813,23 @@ def _row_stride(x: torch.Tensor, what: str) -> int:
     return x.shape[-1] if stride is None else stride
 
 
-def _same_strides(x: torch.Tensor) -> torch.Tensor:
-    return torch.empty_like(x) if x.is_contiguous() else torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device)
+def _dense(x: torch.Tensor) -> torch.Tensor:
+    """An uninitialised contiguous tensor like x (a slice's own elements, not the ones in between)."""
+    return torch.empty_like(x) if x.is_contiguous() else torch.empty(x.shape, dtype=x.dtype, device=x.device)
 
 
 def _like(x: torch.Tensor, t: torch.Tensor, what: str) -> None:
-    if t.dtype != x.dtype or t.shape != x.shape or t.device != x.device or (
-            t.stride() != x.stride() and _row_stride(t, what) != _row_stride(x, "x")):   # (axes of one entry may have any stride)
-        raise ValueError("%s must have the dtype, shape, distance of rows and device of x" % what)
+    if t.dtype != x.dtype or t.shape != x.shape or t.device != x.device:
+        raise ValueError("%s must have the dtype, shape and device of x" % what)
+
+
+def _row_strides(x: torch.Tensor, branch: Optional[torch.Tensor], out: Optional[torch.Tensor], grad: Optional[torch.Tensor],
+                 names: Tuple[str, ...]) -> Optional[BptRowStrides]:
+    """How far the rows of a call's tensors lie apart; None where all are contiguous (as results that the binding makes are: out None)."""
+    given = (x, branch, out, grad)
+    if all(t is None or t.is_contiguous() for t in given):
+        return None
+    return BptRowStrides(*[x.shape[-1] if t is None else _row_stride(t, name) for t, name in zip(given, names)])
 
 
 def _norm_args(x, branch, gate, post, pre, post_gain, post_bias, pre_gain, pre_bias, gate_rows, residual_scale, eps):
@@ -833,7 +851,11 @@ def _norm_args(x, branch, gate, post, pre, post_gain, post_bias, pre_gain, pre_b
     for name, p in (("post_gain", post_gain), ("post_bias", post_bias), ("pre_gain", pre_gain), ("pre_bias", pre_bias)):
         if p is not None and (p.dtype != torch.float32 or tuple(p.shape) != (d,) or not p.is_contiguous() or p.device != dev):
             raise ValueError("%s must be a contiguous float32 tensor [%d] on the device of x" % (name, d))
-    return BptResidualNorm(rows, d, dt, _row_stride(x, "x"), NORMS[post], NORMS[pre], gate_rows, residual_scale, eps)
+    return BptResidualNorm(rows, d, dt, d, NORMS[post], NORMS[pre], gate_rows, residual_scale, eps)
+
+
+def _ref(s: Optional[ctypes.Structure]):
+    return None if s is None else ctypes.byref(s)
 
 
 def bpt_residual_norm_fwd(x: torch.Tensor, branch: Optional[torch.Tensor], gate: Optional[torch.Tensor] = None, post: str = "none",
@@ -841,16 +863,17 @@ def bpt_residual_norm_fwd(x: torch.Tensor, branch: Optional[torch.Tensor], gate:
                           pre_gain: Optional[torch.Tensor] = None, pre_bias: Optional[torch.Tensor] = None, gate_rows: int = 0,
                           residual_scale: float = 1.0, eps: float = 1e-5, want_stats: bool = False):
     """y = residual_scale * x + gate * post(branch) and h = pre(y), post and pre "layer", "rms" or "none" (then h is None).
-    x, branch: [..., d] in fp32 or bf16, equal layouts; gate: [ceil(rows / gate_rows), d] in their type, each row for gate_rows
-    consecutive rows; gains and biases fp32 [d] or None.  Results lie as x does.
+    x, branch: [..., d] in fp32 or bf16, rows evenly apart; gate: [ceil(rows / gate_rows), d] in their type, each row for gate_rows
+    consecutive rows; gains and biases fp32 [d] or None.  Results are contiguous.
     Returns (y, h), with want_stats (y, h, stats) for the backward."""
     s = _norm_args(x, branch, gate, post, pre, post_gain, post_bias, pre_gain, pre_bias, gate_rows, residual_scale, eps)
-    y = _same_strides(x)
-    h = _same_strides(x) if s.pre else None
+    strides = _row_strides(x, branch, None, None, ("x", "branch", "y", "dy"))
+    y = _dense(x)
+    h = _dense(x) if s.pre else None
     stats = torch.empty((s.rows, 4), dtype=torch.float32, device=x.device) if want_stats else None
-    _check(load_library().bpt_residual_norm_fwd(ctypes.byref(s), x.data_ptr(), _ptr(branch), _ptr(gate), _ptr(post_gain), _ptr(post_bias),
-                                                _ptr(pre_gain), _ptr(pre_bias), y.data_ptr(), _ptr(h), _ptr(stats), _raw_stream(x.device.index)),
-           "bpt_residual_norm_fwd")
+    _check(load_library().bpt_residual_norm_fwd_strided(ctypes.byref(s), _ref(strides), x.data_ptr(), _ptr(branch), _ptr(gate), _ptr(post_gain),
+                                                        _ptr(post_bias), _ptr(pre_gain), _ptr(pre_bias), y.data_ptr(), _ptr(h), _ptr(stats),
+                                                        _raw_stream(x.device.index)), "bpt_residual_norm_fwd")
     return (y, h, stats) if want_stats else (y, h)
 
 
@@ -859,8 +882,8 @@ def bpt_residual_norm_bwd(x: torch.Tensor, branch: Optional[torch.Tensor], gate:
                           post_gain: Optional[torch.Tensor] = None, post_bias: Optional[torch.Tensor] = None,
                           pre_gain: Optional[torch.Tensor] = None, pre_bias: Optional[torch.Tensor] = None, gate_rows: int = 0,
                           residual_scale: float = 1.0, eps: float = 1e-5) -> dict:
-    """Backward of bpt_residual_norm_fwd, called with the same arguments and the stats it returned; dy or dh may be None.  Returns
-    a dict: dx, and d_branch, d_gate, d_post_gain, d_post_bias, d_pre_gain, d_pre_bias for what was given."""
+    """Backward of bpt_residual_norm_fwd, called with the same arguments and the stats it returned; dy or dh (rows evenly apart) may
+    be None.  Returns a dict of contiguous tensors: dx, and d_branch, d_gate, d_post_gain, d_post_bias, d_pre_gain, d_pre_bias for what was given."""
     s = _norm_args(x, branch, gate, post, pre, post_gain, post_bias, pre_gain, pre_bias, gate_rows, residual_scale, eps)
     if dy is None and dh is None:
         raise ValueError("pass dy, dh or both")
@@ -869,10 +892,13 @@ def bpt_residual_norm_bwd(x: torch.Tensor, branch: Optional[torch.Tensor], gate:
             _like(x, t, name)
     if stats.dtype != torch.float32 or tuple(stats.shape) != (s.rows, 4) or not stats.is_contiguous() or stats.device != x.device:
         raise ValueError("stats must be what the forward returned")
+    if dy is not None and dh is not None and dy.stride() != dh.stride() and _row_stride(dy, "dy") != _row_stride(dh, "dh"):
+        dy, dh = dy.contiguous(), dh.contiguous()      # (the call has one distance for both)
+    strides = _row_strides(x, branch, None, dh if dy is None else dy, ("x", "branch", "dx", "dy or dh"))
     L = load_library()
-    out = {"dx": _same_strides(x)}
+    out = {"dx": _dense(x)}
     if branch is not None:
-        out["d_branch"] = _same_strides(x)
+        out["d_branch"] = _dense(x)
     for name, p in (("d_gate", gate), ("d_post_gain", post_gain), ("d_post_bias", post_bias), ("d_pre_gain", pre_gain),
                     ("d_pre_bias", pre_bias)):
         if p is not None:
@@ -880,10 +906,10 @@ def bpt_residual_norm_bwd(x: torch.Tensor, branch: Optional[torch.Tensor], gate:
     grads = BptResidualNormGrads(*[_ptr(out.get(n)) for n in ("d_gate", "d_post_gain", "d_post_bias", "d_pre_gain", "d_pre_bias")])
     need = _need(int(L.bpt_residual_norm_bwd_workspace(ctypes.byref(s))), "bpt_residual_norm_bwd_workspace")
     ws, ws_ptr = _workspace(need, x.device)
-    _check(L.bpt_residual_norm_bwd(ctypes.byref(s), x.data_ptr(), _ptr(branch), _ptr(gate), _ptr(post_gain), _ptr(post_bias),
-                                   _ptr(pre_gain), _ptr(pre_bias), stats.data_ptr(), _ptr(dy), _ptr(dh), out["dx"].data_ptr(),
-                                   _ptr(out.get("d_branch")), ctypes.byref(grads), ws_ptr, need, _raw_stream(x.device.index)),
-           "bpt_residual_norm_bwd")
+    _check(L.bpt_residual_norm_bwd_strided(ctypes.byref(s), _ref(strides), x.data_ptr(), _ptr(branch), _ptr(gate), _ptr(post_gain),
+                                           _ptr(post_bias), _ptr(pre_gain), _ptr(pre_bias), stats.data_ptr(), _ptr(dy), _ptr(dh),
+                                           out["dx"].data_ptr(), _ptr(out.get("d_branch")), ctypes.byref(grads), ws_ptr, need,
+                                           _raw_stream(x.device.index)), "bpt_residual_norm_bwd")
     return out
 
 
@@ -898,50 +924,62 @@ def _ffn_args(X, Wg, Wu, Wd, activation, bf16_grads=False):
     for name, W, shape in (("Wg", Wg, (d, f)), ("Wu", Wu, (d, f)), ("Wd", Wd, (f, d))):
         if W.dtype != torch.bfloat16 or tuple(W.shape) != shape or not W.is_contiguous() or W.device != dev:
             raise ValueError("%s must be a contiguous bfloat16 tensor %s on the device of X" % (name, shape))
-    return BptGatedFfn(X.numel() // d if d else 0, d, f, BPT_BF16, ACTIVATIONS[activation], _row_stride(X, "X"),
-                       BPT_BF16 if bf16_grads else BPT_F32)
+    return BptGatedFfn(X.numel() // d if d else 0, d, f, BPT_BF16, ACTIVATIONS[activation], d, BPT_BF16 if bf16_grads else BPT_F32)
 
 
 def bpt_gated_ffn_fwd(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.Tensor, activation: str = "silu",
                       out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """Y = (act(X Wg) * (X Wu)) Wd for X [..., d] bf16, Wg, Wu [d, f], Wd [f, d]; act "silu", "gelu" or "relu"."""
+    """Y = (act(X Wg) * (X Wu)) Wd for X [..., d] bf16, rows evenly apart, Wg, Wu [d, f], Wd [f, d]; act "silu", "gelu" or "relu".  Y is
+    contiguous, or `out`, whose rows lie evenly apart."""
     s = _ffn_args(X, Wg, Wu, Wd, activation)
     L = load_library()
-    if out is None:
-        out = _same_strides(X)
-    else:
+    if out is not None:
         _like(X, out, "out")
+    strides = _row_strides(X, None, out, None, ("X", "", "out", ""))
+    if out is None:
+        out = _dense(X)
     need = _need(int(L.bpt_gated_ffn_fwd_workspace(ctypes.byref(s))), "bpt_gated_ffn_fwd_workspace")
     if workspace is None:
         workspace = torch.empty(need, dtype=torch.uint8, device=X.device)
-    _check(L.bpt_gated_ffn_fwd(ctypes.byref(s), X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(), out.data_ptr(),
-                               workspace.data_ptr(), workspace.numel() * workspace.element_size(), _raw_stream(X.device.index)), "bpt_gated_ffn_fwd")
+    _check(L.bpt_gated_ffn_fwd_strided(ctypes.byref(s), _ref(strides), X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(), out.data_ptr(),
+                                       workspace.data_ptr(), workspace.numel() * workspace.element_size(), _raw_stream(X.device.index)),
+           "bpt_gated_ffn_fwd")
     return out
 
 
 def bpt_gated_ffn_bwd(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.Tensor, dY: torch.Tensor, activation: str = "silu",
                       bf16_grads: bool = False, workspace: Optional[torch.Tensor] = None):
-    """Backward of bpt_gated_ffn_fwd, which forms the hidden activations again: (dX, dWg, dWu, dWd), the weights' gradients in fp32 or,
-    with bf16_grads, rounded to bf16."""
+    """Backward of bpt_gated_ffn_fwd, which forms the hidden activations again: (dX, dWg, dWu, dWd), contiguous, the weights' gradients
+    in fp32 or, with bf16_grads, rounded to bf16.  dY: rows evenly apart."""
     s = _ffn_args(X, Wg, Wu, Wd, activation, bf16_grads)
     _like(X, dY, "dY")
+    strides = _row_strides(X, None, None, dY, ("X", "", "", "dY"))
     L = load_library()
-    dX = _same_strides(X)
+    dX = _dense(X)
     dWg, dWu, dWd = (torch.empty(W.shape, dtype=torch.bfloat16 if bf16_grads else torch.float32, device=X.device) for W in (Wg, Wu, Wd))
     need = _need(int(L.bpt_gated_ffn_bwd_workspace(ctypes.byref(s))), "bpt_gated_ffn_bwd_workspace")
     if workspace is None:
         workspace = torch.empty(need, dtype=torch.uint8, device=X.device)
-    _check(L.bpt_gated_ffn_bwd(ctypes.byref(s), X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(), dY.data_ptr(), dX.data_ptr(),
-                               dWg.data_ptr(), dWu.data_ptr(), dWd.data_ptr(), workspace.data_ptr(),
-                               workspace.numel() * workspace.element_size(), _raw_stream(X.device.index)), "bpt_gated_ffn_bwd")
+    _check(L.bpt_gated_ffn_bwd_strided(ctypes.byref(s), _ref(strides), X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(), dY.data_ptr(),
+                                       dX.data_ptr(), dWg.data_ptr(), dWu.data_ptr(), dWd.data_ptr(), workspace.data_ptr(),
+                                       workspace.numel() * workspace.element_size(), _raw_stream(X.device.index)), "bpt_gated_ffn_bwd")
     return dX, dWg, dWu, dWd
 
 
-def _in_layout_of(x: torch.Tensor, g: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
-    """A gradient with the strides and dtype of x on a 16-byte boundary, as the calls ask for (autograd hands over any)."""
-    if g is None or (g.stride() == x.stride() and g.dtype == x.dtype and not g.data_ptr() & 15):
-        return g
-    return torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device).copy_(g)
+def _even_rows(x: torch.Tensor) -> bool:
+    """Whether the row operators take x [..., d] as it lies."""
+    if x.is_contiguous():
+        return not x.data_ptr() & 15
+    try:
+        stride = _row_stride(x, "a gradient")
+    except ValueError:
+        return False
+    return stride >= x.shape[-1] and not stride & 7 and not x.data_ptr() & 15
+
+
+def _gradient(x: torch.Tensor, g: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
+    """A gradient of x's dtype that the row operators take (autograd hands over any layout and place)."""
+    return g if g is None or (g.dtype == x.dtype and _even_rows(g)) else _dense(x).copy_(g)
 
 
 def _rows_usable(x: torch.Tensor) -> bool:
@@ -997,7 +1035,7 @@ class ResidualNormFunction(torch.autograd.Function):
         x, branch, gate, stats, post_gain, post_bias, pre_gain, pre_bias = ctx.saved_tensors
         if dy is None and dh is None:
             return (None,) * 8
-        g = bpt_residual_norm_bwd(x, branch, gate, stats, _in_layout_of(x, dy), _in_layout_of(x, dh), post_gain=post_gain,
+        g = bpt_residual_norm_bwd(x, branch, gate, stats, _gradient(x, dy), _gradient(x, dh), post_gain=post_gain,
                                   post_bias=post_bias, pre_gain=pre_gain, pre_bias=pre_bias, **ctx.how)
         return (g["dx"],) + tuple(g.get("d_" + n) for n in ("branch", "gate", "post_gain", "post_bias", "pre_gain", "pre_bias")) + (None,)
 
@@ -1024,7 +1062,7 @@ class GatedFfnFunction(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dY):
         X, Wg, Wu, Wd = ctx.saved_tensors
-        return bpt_gated_ffn_bwd(X, Wg, Wu, Wd, _in_layout_of(X, dY), ctx.activation, bf16_grads=True) + (None,)
+        return bpt_gated_ffn_bwd(X, Wg, Wu, Wd, _gradient(X, dY), ctx.activation, bf16_grads=True) + (None,)
 
 
 def gated_ffn(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.Tensor, activation: str = "silu") -> torch.Tensor:

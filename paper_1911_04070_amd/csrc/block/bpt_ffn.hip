@@ -340,7 +340,7 @@ __global__ void __launch_bounds__(C::kThreads) product_sum_kernel(const ProductA
 struct HiddenArgs {
     const bf16_t *X, *dY, *Wg, *Wu, *Wd;
     bf16_t *F, *dG, *dU;
-    int64_t M, ldx;
+    int64_t M, ldx, ldy;   // (ldy: of dY)
     int32_t d, f, tiles_m, tiles_n;
 };
 // G = X Wg and U = X Wu are formed again, then dF = dY Wd^T on the same tile: F, dG and dU are written, rounded once.  G and U could
@@ -370,9 +370,9 @@ __global__ void __launch_bounds__(C::kThreads, C::kWavesPerSimd) gated_hidden_bw
         });
     }
     C2 t;
-    t.init(shared, g.ldx, g.M - m0, g.d, g.f - n0);
+    t.init(shared, g.ldy, g.M - m0, g.d, g.f - n0);
     typename C2::Acc df = {};
-    const bf16_t *dY = g.dY + m0 * g.ldx, *Wd = g.Wd + (int64_t)n0 * g.d;
+    const bf16_t *dY = g.dY + m0 * g.ldy, *Wd = g.Wd + (int64_t)n0 * g.d;
     t.run(df, slabs, [&](int s, const bf16_t*& a, const bf16_t*& b0, const bf16_t*& b1, int64_t& k_left) {
         a = dY + s * C::kSlab;
         b0 = Wd + s * C::kSlab;
@@ -569,11 +569,12 @@ int launch_hidden(HiddenArgs& g, hipStream_t st) {
     return launch_hidden_as<ACT, Tile<64, 128, 2, 2, 128, 2, true, false, true>, Tile<64, 64, 2, 2, 128, 2, true, true, false>>(g, st);
 }
 
+constexpr int64_t kMostStride = ((int64_t)1 << 20) - 1;   // (offsets within a tile are 32 bits)
 int check_ffn(const bpt_gated_ffn_t* s) {
     if (!s || s->rows < 0) return BPT_ERR_INVALID_ARG;
     if (s->dtype != BPT_BF16 || s->rows >= INT32_MAX) return BPT_ERR_UNSUPPORTED;
     if (s->d < 8 || s->f < 8 || (s->d & 7) || (s->f & 7) || s->d > 65536 || s->f > 65536) return BPT_ERR_UNSUPPORTED;
-    if (s->stride < s->d || (s->stride & 7) || s->stride >= ((int64_t)1 << 20)) return BPT_ERR_INVALID_ARG;
+    if (!stride_ok(s->stride, s->d, kMostStride)) return BPT_ERR_INVALID_ARG;
     if (s->activation < BPT_ACT_SILU || s->activation > BPT_ACT_RELU) return BPT_ERR_INVALID_ARG;
     if (s->grad_dtype != BPT_F32 && s->grad_dtype != BPT_BF16) return BPT_ERR_INVALID_ARG;
     // a launch has fewer than 2^32 threads, 512 for a tile at most
@@ -631,27 +632,29 @@ BwdBuffers bwd_buffers(const bpt_gated_ffn_t* s) {
     return b;
 }
 
-ProductArgs wd_product(const bpt_gated_ffn_t* s, const bf16_t* F, const bf16_t* dY, void* dWd) {
+ProductArgs wd_product(const bpt_gated_ffn_t* s, const bpt_row_strides_t& apart, const bf16_t* F, const bf16_t* dY, void* dWd) {
     ProductArgs g = {};
     g.A[0] = g.A[1] = F; g.B[0] = g.B[1] = dY; g.C[0] = g.C[1] = dWd;
     g.M = s->f; g.N = s->d; g.K = s->rows;
-    g.lda = s->f; g.ldb = s->stride; g.ldc = s->d;
+    g.lda = s->f; g.ldb = apart.grad; g.ldc = s->d;
     g.terms = g.matrices = 1;
     return g;
 }
-ProductArgs wgu_product(const bpt_gated_ffn_t* s, const bf16_t* X, const bf16_t* dG, const bf16_t* dU, void* dWg, void* dWu) {
+ProductArgs wgu_product(const bpt_gated_ffn_t* s, const bpt_row_strides_t& apart, const bf16_t* X, const bf16_t* dG, const bf16_t* dU, void* dWg,
+                        void* dWu) {
     ProductArgs g = {};
     g.A[0] = g.A[1] = X; g.B[0] = dG; g.B[1] = dU; g.C[0] = dWg; g.C[1] = dWu;
     g.M = s->d; g.N = s->f; g.K = s->rows;
-    g.lda = s->stride; g.ldb = s->f; g.ldc = s->f;
+    g.lda = apart.x; g.ldb = s->f; g.ldc = s->f;
     g.terms = 1; g.matrices = 2;
     return g;
 }
-ProductArgs dx_product(const bpt_gated_ffn_t* s, const bf16_t* dG, const bf16_t* dU, const bf16_t* Wg, const bf16_t* Wu, void* dX) {
+ProductArgs dx_product(const bpt_gated_ffn_t* s, const bpt_row_strides_t& apart, const bf16_t* dG, const bf16_t* dU, const bf16_t* Wg,
+                       const bf16_t* Wu, void* dX) {
     ProductArgs g = {};
     g.A[0] = dG; g.A[1] = dU; g.B[0] = Wg; g.B[1] = Wu; g.C[0] = g.C[1] = dX;
     g.M = s->rows; g.N = s->d; g.K = s->f;
-    g.lda = g.ldb = s->f; g.ldc = s->stride;
+    g.lda = g.ldb = s->f; g.ldc = apart.out;
     g.terms = 2; g.matrices = 1;
     return g;
 }
@@ -736,10 +739,12 @@ size_t bpt_gated_ffn_fwd_workspace(const bpt_gated_ffn_t* s) {
     return fwd_buffers(s).total;
 }
 
-int bpt_gated_ffn_fwd(const bpt_gated_ffn_t* s, const void* X, const void* Wg, const void* Wu, const void* Wd, void* Y, void* workspace,
-                      size_t workspace_bytes, void* stream) {
+int bpt_gated_ffn_fwd_strided(const bpt_gated_ffn_t* s, const bpt_row_strides_t* strides, const void* X, const void* Wg, const void* Wu,
+                              const void* Wd, void* Y, void* workspace, size_t workspace_bytes, void* stream) {
     if (const int rc = check_ffn(s)) return rc;
     if (s->rows == 0) return BPT_OK;
+    const bpt_row_strides_t apart = row_strides(strides, s->stride);
+    if (!stride_ok(apart.x, s->d, kMostStride) || !stride_ok(apart.out, s->d, kMostStride)) return BPT_ERR_INVALID_ARG;
     if (!X || !Wg || !Wu || !Wd || !Y || !workspace || off_boundary(X, Wg, Wu, Wd, Y, workspace)) return BPT_ERR_INVALID_ARG;
     const FwdBuffers b = fwd_buffers(s);
     if (workspace_bytes < b.total) return BPT_ERR_INVALID_ARG;
@@ -750,12 +755,12 @@ int bpt_gated_ffn_fwd(const bpt_gated_ffn_t* s, const void* X, const void* Wg, c
     u.X = static_cast<const bf16_t*>(X); u.Wg = static_cast<const bf16_t*>(Wg); u.Wu = static_cast<const bf16_t*>(Wu);
     u.F = F;
     u.F_low = b.up_strips && b.down_strips ? reinterpret_cast<bf16_t*>(ws + b.F_low) : nullptr;
-    u.M = s->rows; u.ldx = s->stride; u.d = s->d; u.f = s->f;
+    u.M = s->rows; u.ldx = apart.x; u.d = s->d; u.f = s->f;
     const int rc = s->activation == BPT_ACT_SILU ? launch_up<BPT_ACT_SILU>(u, st)
                    : s->activation == BPT_ACT_GELU ? launch_up<BPT_ACT_GELU>(u, st) : launch_up<BPT_ACT_RELU>(u, st);
     if (rc) return rc;
     if (b.down_strips) {
-        const DownArgs g = {{F, u.F_low}, static_cast<const bf16_t*>(Wd), static_cast<bf16_t*>(Y), s->rows, s->stride, s->d, s->f, b.slices, b.slice_k,
+        const DownArgs g = {{F, u.F_low}, static_cast<const bf16_t*>(Wd), static_cast<bf16_t*>(Y), s->rows, apart.out, s->d, s->f, b.slices, b.slice_k,
                             reinterpret_cast<float*>(ws + b.part)};
         dim3 grid = strip_grid(s->rows, s->d);
         grid.z = b.slices;
@@ -773,9 +778,14 @@ int bpt_gated_ffn_fwd(const bpt_gated_ffn_t* s, const void* X, const void* Wg, c
     ProductArgs g = {};
     g.A[0] = g.A[1] = F; g.B[0] = g.B[1] = static_cast<const bf16_t*>(Wd); g.C[0] = g.C[1] = Y;
     g.M = s->rows; g.N = s->d; g.K = s->f;
-    g.lda = s->f; g.ldb = s->d; g.ldc = s->stride;
+    g.lda = s->f; g.ldb = s->d; g.ldc = apart.out;
     g.terms = g.matrices = 1;
     return launch_product<true, false, bf16_t>(g, b.down, ws + b.part, st);
+}
+
+int bpt_gated_ffn_fwd(const bpt_gated_ffn_t* s, const void* X, const void* Wg, const void* Wu, const void* Wd, void* Y, void* workspace,
+                      size_t workspace_bytes, void* stream) {
+    return bpt_gated_ffn_fwd_strided(s, nullptr, X, Wg, Wu, Wd, Y, workspace, workspace_bytes, stream);
 }
 
 size_t bpt_gated_ffn_bwd_workspace(const bpt_gated_ffn_t* s) {
@@ -783,9 +793,11 @@ size_t bpt_gated_ffn_bwd_workspace(const bpt_gated_ffn_t* s) {
     return bwd_buffers(s).total;
 }
 
-int bpt_gated_ffn_bwd(const bpt_gated_ffn_t* s, const void* X, const void* Wg, const void* Wu, const void* Wd, const void* dY, void* dX,
-                      void* dWg, void* dWu, void* dWd, void* workspace, size_t workspace_bytes, void* stream) {
+int bpt_gated_ffn_bwd_strided(const bpt_gated_ffn_t* s, const bpt_row_strides_t* strides, const void* X, const void* Wg, const void* Wu,
+                              const void* Wd, const void* dY, void* dX, void* dWg, void* dWu, void* dWd, void* workspace,
+                              size_t workspace_bytes, void* stream) {
     if (const int rc = check_ffn(s)) return rc;
+    const bpt_row_strides_t apart = row_strides(strides, s->stride);
     if (!Wg || !Wu || !Wd || !dWg || !dWu || !dWd || off_boundary(X, Wg, Wu, Wd, dY, dX, dWg, dWu, dWd, workspace)) return BPT_ERR_INVALID_ARG;
     const BwdBuffers b = bwd_buffers(s);
     hipStream_t st = static_cast<hipStream_t>(stream);
@@ -793,23 +805,31 @@ int bpt_gated_ffn_bwd(const bpt_gated_ffn_t* s, const void* X, const void* Wg, c
     const bf16_t *x = static_cast<const bf16_t*>(X), *dy = static_cast<const bf16_t*>(dY);
     if (s->rows > 0) {
         if (!X || !dY || !dX || !workspace || workspace_bytes < b.total) return BPT_ERR_INVALID_ARG;
+        for (int64_t x : {apart.x, apart.out, apart.grad})
+            if (!stride_ok(x, s->d, kMostStride)) return BPT_ERR_INVALID_ARG;
+        if (!same_place(dX, dY, s->rows, apart.out, apart.grad) || !same_place(dX, X, s->rows, apart.out, apart.x)) return BPT_ERR_INVALID_ARG;
         HiddenArgs h = {};
         h.X = x; h.dY = dy;
         h.Wg = static_cast<const bf16_t*>(Wg); h.Wu = static_cast<const bf16_t*>(Wu); h.Wd = static_cast<const bf16_t*>(Wd);
         h.F = reinterpret_cast<bf16_t*>(ws + b.F);
         h.dG = reinterpret_cast<bf16_t*>(ws + b.dG);
         h.dU = reinterpret_cast<bf16_t*>(ws + b.dU);
-        h.M = s->rows; h.ldx = s->stride; h.d = s->d; h.f = s->f;
+        h.M = s->rows; h.ldx = apart.x; h.ldy = apart.grad; h.d = s->d; h.f = s->f;
         const int rc = s->activation == BPT_ACT_SILU ? launch_hidden<BPT_ACT_SILU>(h, st)
                        : s->activation == BPT_ACT_GELU ? launch_hidden<BPT_ACT_GELU>(h, st) : launch_hidden<BPT_ACT_RELU>(h, st);
         if (rc) return rc;
     }
     const bf16_t *F = reinterpret_cast<const bf16_t*>(ws + b.F), *dG = reinterpret_cast<const bf16_t*>(ws + b.dG),
                  *dU = reinterpret_cast<const bf16_t*>(ws + b.dU);
-    GradArgs g = {dx_product(s, dG, dU, static_cast<const bf16_t*>(Wg), static_cast<const bf16_t*>(Wu), dX),
-                  wgu_product(s, x, dG, dU, dWg, dWu), wd_product(s, F, dy, dWd), 0};
+    GradArgs g = {dx_product(s, apart, dG, dU, static_cast<const bf16_t*>(Wg), static_cast<const bf16_t*>(Wu), dX),
+                  wgu_product(s, apart, x, dG, dU, dWg, dWu), wd_product(s, apart, F, dy, dWd), 0};
     const bool dx_alone = dX == dY || dX == X;
     return s->grad_dtype == BPT_BF16 ? grads<bf16_t>(s, b, g, dx_alone, ws + b.part, st) : grads<float>(s, b, g, dx_alone, ws + b.part, st);
+}
+
+int bpt_gated_ffn_bwd(const bpt_gated_ffn_t* s, const void* X, const void* Wg, const void* Wu, const void* Wd, const void* dY, void* dX,
+                      void* dWg, void* dWu, void* dWd, void* workspace, size_t workspace_bytes, void* stream) {
+    return bpt_gated_ffn_bwd_strided(s, nullptr, X, Wg, Wu, Wd, dY, dX, dWg, dWu, dWd, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

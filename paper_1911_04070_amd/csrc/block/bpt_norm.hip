@@ -25,7 +25,8 @@ struct NormArgs {
     void* d_gate;          // written by the row kernel where a gate row has one slice, else by the sum over slices
     float* gate_part;      // [units][d]: sums of a slice of a gate row's rows
     float* part;           // [gridDim.x][sums][d]: sums over a workgroup's rows
-    int64_t rows, stride, gate_rows;
+    int64_t rows, gate_rows;
+    bpt_row_strides_t stride;
     int32_t d, post, pre;
     float residual_scale, eps;
     // a workgroup takes units blockIdx.x, + gridDim.x, ..: unit u is slice u % slices of the rows of gate row u / slices
@@ -122,8 +123,8 @@ __global__ void __launch_bounds__(RowTeam<THREADS>::kBlock, sizeof(T) == 2 ? 5 :
     Raw8<T> xw = {}, bw = {}, gw = {};
     auto fetch = [&](int64_t r) {
         if (!has || r >= a.rows) return;
-        xw.load(px + r * a.stride + col);
-        if (pb) bw.load(pb + r * a.stride + col);
+        xw.load(px + r * a.stride.x + col);
+        if (pb) bw.load(pb + r * a.stride.branch + col);
         if (pg) gw.load(pg + (int64_t)((uint32_t)r / (uint32_t)a.gate_rows) * a.d + col);
     };
     fetch(row);
@@ -145,11 +146,11 @@ __global__ void __launch_bounds__(RowTeam<THREADS>::kBlock, sizeof(T) == 2 ? 5 :
         }
         if (a.pre != BPT_NORM_NONE) sy = row_stats<THREADS>(x, has, a.pre, inv_d, a.eps, lds, slot);
         if (!live) continue;
-        if (a.y) store8(static_cast<T*>(a.y) + row * a.stride + col, x);
+        if (a.y) store8(static_cast<T*>(a.y) + row * a.stride.out + col, x);
         if (a.pre != BPT_NORM_NONE) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = (x[e] - sy.x) * sy.y * g2[e] + b2[e];
-            store8(static_cast<T*>(a.h) + row * a.stride + col, x);
+            store8(static_cast<T*>(a.h) + row * a.stride.out + col, x);
         }
         if (a.stats_out && col == 0) a.stats_out[row] = make_float4(sb.x, sb.y, sy.x, sy.y);
     }
@@ -163,6 +164,12 @@ __global__ void __launch_bounds__(RowTeam<THREADS>::kBlock, sizeof(T) == 2 ? 5 :
 // fp32 as the forward did, not from its rounded copy), six values of memory traffic per element; the sums stay in the
 // thread's registers over all rows of its workgroup, which leaves two wavefronts per SIMD: rows have to be requested early.
 // 65 532 rows of 512 in bf16: 93 us, 4.3 TB/s (one row ahead instead of two: 100 us); 4095 rows of 2048 in fp32: 40 us, 5.0 TB/s.
+// A row's number as a new value to the compiler, which else keeps a running offset in registers for every tensor and row on its way
+// (with strides of their own for the tensors 256 registers and up to 9 spilled; so 218 to 240 and none)
+__device__ __forceinline__ uint32_t hidden(uint32_t v) {
+    asm("" : "+v"(v));
+    return v;
+}
 template <typename T, int THREADS>
 __global__ void __launch_bounds__(RowTeam<THREADS>::kBlock, 2) residual_norm_bwd_kernel(const NormArgs a) {
     using Team = RowTeam<THREADS>;
@@ -211,12 +218,13 @@ __global__ void __launch_bounds__(RowTeam<THREADS>::kBlock, 2) residual_norm_bwd
             if (r >= end) return;
             w.st = a.stats[r];
             if (!has) return;
-            const int64_t at = r * a.stride + col;
-            w.x.load(px + at);
-            if (pb) w.b.load(pb + at);
+            const uint32_t at_row = hidden((uint32_t)r);
+            w.x.load(px + at_row * a.stride.x + col);
+            if (pb) w.b.load(pb + at_row * a.stride.branch + col);
+            const int64_t at = at_row * a.stride.grad + col;
             if (pdy) w.dy.load(pdy + at);
             if (pdh) w.dh.load(pdh + at);
-            if (gate_each) w.g.load(pg + r * a.d + col);
+            if (gate_each) w.g.load(pg + at_row * (int64_t)a.d + col);
         };
         auto work = [&](Row& w, int64_t row) {
             const bool live = has && row < end;
@@ -262,14 +270,14 @@ __global__ void __launch_bounds__(RowTeam<THREADS>::kBlock, 2) residual_norm_bwd
                 float o[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) o[e] = a.residual_scale * dy[e];
-                store8(static_cast<T*>(a.dx) + row * a.stride + col, o);
+                store8(static_cast<T*>(a.dx) + hidden((uint32_t)row) * a.stride.out + col, o);
             }
             if (pg) {
                 if (gate_each) {
                     float o[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) o[e] = dy[e] * bn[e];
-                    if (live) store8(static_cast<T*>(a.d_gate) + row * a.d + col, o);
+                    if (live) store8(static_cast<T*>(a.d_gate) + hidden((uint32_t)row) * (int64_t)a.d + col, o);
                 } else if (live) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) sum_gate[e] += dy[e] * bn[e];
@@ -295,7 +303,7 @@ __global__ void __launch_bounds__(RowTeam<THREADS>::kBlock, 2) residual_norm_bwd
 #pragma unroll
                 for (int e = 0; e < 8; ++e) dy[e] = s.y * (dy[e] * g1[e] - m1 - b[e] * m2);
             }
-            if (live && a.d_branch) store8(static_cast<T*>(a.d_branch) + row * a.stride + col, dy);
+            if (live && a.d_branch) store8(static_cast<T*>(a.d_branch) + hidden((uint32_t)row) * a.stride.out + col, dy);
         };
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) fetch(rows[i], begin + team + i * Team::kRows);
@@ -378,11 +386,12 @@ int norm_threads(int d) {
     return t;
 }
 
+constexpr int64_t kMostStride = (int64_t)1 << 40;
 int check_norm(const bpt_residual_norm_t* s) {
     if (!s || s->rows < 0) return BPT_ERR_INVALID_ARG;
     if (s->dtype != BPT_F32 && s->dtype != BPT_BF16) return BPT_ERR_UNSUPPORTED;
     if (s->d < 8 || s->d > 4096 || (s->d & 7) || s->rows >= INT32_MAX) return BPT_ERR_UNSUPPORTED;
-    if (s->stride < s->d || (s->stride & 7) || s->stride > ((int64_t)1 << 40)) return BPT_ERR_INVALID_ARG;
+    if (!stride_ok(s->stride, s->d, kMostStride)) return BPT_ERR_INVALID_ARG;
     for (int k : {s->post, s->pre})
         if (k != BPT_NORM_NONE && k != BPT_NORM_LAYER && k != BPT_NORM_RMS) return BPT_ERR_INVALID_ARG;
     if (s->gate_rows < 0 || s->gate_rows >= INT32_MAX || !std::isfinite(s->residual_scale) || !std::isfinite(s->eps)) return BPT_ERR_INVALID_ARG;
@@ -467,20 +476,24 @@ int launch_bwd_any(const NormArgs& a, int blocks, hipStream_t st) {
     }
 }
 
-NormArgs norm_args(const bpt_residual_norm_t* s, const void* x, const void* branch, const void* gate, const float* post_gain,
+NormArgs norm_args(const bpt_residual_norm_t* s, const bpt_row_strides_t& strides, const void* x, const void* branch, const void* gate, const float* post_gain,
                    const float* post_bias, const float* pre_gain, const float* pre_bias) {
     NormArgs a = {};
+    a.stride = strides;
     a.x = x; a.branch = branch; a.gate = gate;
     a.post_gain = post_gain; a.post_bias = post_bias; a.pre_gain = pre_gain; a.pre_bias = pre_bias;
-    a.rows = s->rows; a.stride = s->stride; a.gate_rows = std::max<int64_t>(s->gate_rows, 1);
+    a.rows = s->rows; a.gate_rows = std::max<int64_t>(s->gate_rows, 1);
     a.d = s->d; a.post = s->post; a.pre = s->pre;
     a.residual_scale = s->residual_scale;
     a.eps = s->eps > 0.f ? s->eps : 1e-5f;
     return a;
 }
 // what both calls ask of their inputs
-int check_inputs(const bpt_residual_norm_t* s, const void* x, const void* branch, const void* gate, const float* post_gain,
+int check_inputs(const bpt_residual_norm_t* s, const bpt_row_strides_t& strides, const void* x, const void* branch, const void* gate, const float* post_gain,
                  const float* post_bias, const float* pre_gain, const float* pre_bias) {
+    if (!stride_ok(strides.x, s->d, kMostStride) || !stride_ok(strides.out, s->d, kMostStride) ||
+        (branch && !stride_ok(strides.branch, s->d, kMostStride)))
+        return BPT_ERR_INVALID_ARG;
     if (!x || !gate != (s->gate_rows == 0)) return BPT_ERR_INVALID_ARG;
     if (!branch && (gate || s->post != BPT_NORM_NONE)) return BPT_ERR_INVALID_ARG;
     if (s->post == BPT_NORM_NONE && (post_gain || post_bias)) return BPT_ERR_INVALID_ARG;
@@ -495,18 +508,27 @@ using namespace bpt;
 
 extern "C" {
 
-int bpt_residual_norm_fwd(const bpt_residual_norm_t* s, const void* x, const void* branch, const void* gate, const float* post_gain,
-                          const float* post_bias, const float* pre_gain, const float* pre_bias, void* y, void* h, float* stats,
-                          void* stream) {
+int bpt_residual_norm_fwd_strided(const bpt_residual_norm_t* s, const bpt_row_strides_t* strides, const void* x, const void* branch,
+                                  const void* gate, const float* post_gain, const float* post_bias, const float* pre_gain,
+                                  const float* pre_bias, void* y, void* h, float* stats, void* stream) {
     if (const int rc = check_norm(s)) return rc;
     if (s->rows == 0) return BPT_OK;
-    if (const int rc = check_inputs(s, x, branch, gate, post_gain, post_bias, pre_gain, pre_bias)) return rc;
+    const bpt_row_strides_t apart = row_strides(strides, s->stride);
+    if (const int rc = check_inputs(s, apart, x, branch, gate, post_gain, post_bias, pre_gain, pre_bias)) return rc;
     if (!h != (s->pre == BPT_NORM_NONE) || (!y && !h) || y == h || off_boundary(y, h, stats)) return BPT_ERR_INVALID_ARG;
-    NormArgs a = norm_args(s, x, branch, gate, post_gain, post_bias, pre_gain, pre_bias);
+    for (const void* o : {y, h})
+        if (!same_place(o, x, s->rows, apart.out, apart.x) || !same_place(o, branch, s->rows, apart.out, apart.branch)) return BPT_ERR_INVALID_ARG;
+    NormArgs a = norm_args(s, apart, x, branch, gate, post_gain, post_bias, pre_gain, pre_bias);
     a.y = y; a.h = h;
     a.stats_out = reinterpret_cast<float4*>(stats);
     hipStream_t st = static_cast<hipStream_t>(stream);
     return s->dtype == BPT_BF16 ? launch_fwd_any<bf16_t>(a, st) : launch_fwd_any<float>(a, st);
+}
+
+int bpt_residual_norm_fwd(const bpt_residual_norm_t* s, const void* x, const void* branch, const void* gate, const float* post_gain,
+                          const float* post_bias, const float* pre_gain, const float* pre_bias, void* y, void* h, float* stats,
+                          void* stream) {
+    return bpt_residual_norm_fwd_strided(s, nullptr, x, branch, gate, post_gain, post_bias, pre_gain, pre_bias, y, h, stats, stream);
 }
 
 size_t bpt_residual_norm_bwd_workspace(const bpt_residual_norm_t* s) {
@@ -514,11 +536,12 @@ size_t bpt_residual_norm_bwd_workspace(const bpt_residual_norm_t* s) {
     return s->rows == 0 ? 0 : bwd_plan(s).total;
 }
 
-int bpt_residual_norm_bwd(const bpt_residual_norm_t* s, const void* x, const void* branch, const void* gate, const float* post_gain,
-                          const float* post_bias, const float* pre_gain, const float* pre_bias, const float* stats, const void* dy,
-                          const void* dh, void* dx, void* d_branch, const bpt_residual_norm_grads_t* grads, void* workspace,
-                          size_t workspace_bytes, void* stream) {
+int bpt_residual_norm_bwd_strided(const bpt_residual_norm_t* s, const bpt_row_strides_t* strides, const void* x, const void* branch,
+                                  const void* gate, const float* post_gain, const float* post_bias, const float* pre_gain,
+                                  const float* pre_bias, const float* stats, const void* dy, const void* dh, void* dx, void* d_branch,
+                                  const bpt_residual_norm_grads_t* grads, void* workspace, size_t workspace_bytes, void* stream) {
     if (const int rc = check_norm(s)) return rc;
+    const bpt_row_strides_t apart = row_strides(strides, s->stride);
     if (!grads) return BPT_ERR_INVALID_ARG;
     float* const out[4] = {grads->d_post_gain, grads->d_post_bias, grads->d_pre_gain, grads->d_pre_bias};
     const float* const par[4] = {post_gain, post_bias, pre_gain, pre_bias};
@@ -526,7 +549,7 @@ int bpt_residual_norm_bwd(const bpt_residual_norm_t* s, const void* x, const voi
         if (!out[i] != !par[i] || off_boundary(out[i])) return BPT_ERR_INVALID_ARG;
     hipStream_t st = static_cast<hipStream_t>(stream);
     SumJobs j = {};
-    NormArgs a = norm_args(s, x, branch, gate, post_gain, post_bias, pre_gain, pre_bias);
+    NormArgs a = norm_args(s, apart, x, branch, gate, post_gain, post_bias, pre_gain, pre_bias);
     for (int i = 0; i < 4; ++i) {
         a.sum_at[i] = out[i] ? j.num_sums : -1;
         if (out[i]) j.out[j.num_sums++] = out[i];
@@ -534,10 +557,13 @@ int bpt_residual_norm_bwd(const bpt_residual_norm_t* s, const void* x, const voi
     j.d = s->d;
     int64_t gate_jobs = 0;
     if (s->rows > 0) {
-        if (const int rc = check_inputs(s, x, branch, gate, post_gain, post_bias, pre_gain, pre_bias)) return rc;
+        if (const int rc = check_inputs(s, apart, x, branch, gate, post_gain, post_bias, pre_gain, pre_bias)) return rc;
         if (!stats || !dx || !d_branch != !branch || !grads->d_gate != !gate || (dh && s->pre == BPT_NORM_NONE) || (!dy && !dh) ||
             dx == d_branch || off_boundary(stats, dy, dh, dx, d_branch, grads->d_gate, workspace))
             return BPT_ERR_INVALID_ARG;
+        if (!stride_ok(apart.grad, s->d, kMostStride)) return BPT_ERR_INVALID_ARG;
+        for (const void* g : {dy, dh})
+            if (!same_place(dx, g, s->rows, apart.out, apart.grad) || !same_place(d_branch, g, s->rows, apart.out, apart.grad)) return BPT_ERR_INVALID_ARG;
         const BwdPlan p = bwd_plan(s);
         if (!workspace || workspace_bytes < p.total) return BPT_ERR_INVALID_ARG;
         unsigned char* ws = static_cast<unsigned char*>(workspace);
@@ -563,6 +589,14 @@ int bpt_residual_norm_bwd(const bpt_residual_norm_t* s, const void* x, const voi
     else BPT_LAUNCH("norm_column_sum_kernel", norm_column_sum_kernel<float>, grid, dim3(256), 0, st, j);
     BPT_HIP(hipGetLastError());
     return BPT_OK;
+}
+
+int bpt_residual_norm_bwd(const bpt_residual_norm_t* s, const void* x, const void* branch, const void* gate, const float* post_gain,
+                          const float* post_bias, const float* pre_gain, const float* pre_bias, const float* stats, const void* dy,
+                          const void* dh, void* dx, void* d_branch, const bpt_residual_norm_grads_t* grads, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+    return bpt_residual_norm_bwd_strided(s, nullptr, x, branch, gate, post_gain, post_bias, pre_gain, pre_bias, stats, dy, dh, dx, d_branch,
+                                         grads, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

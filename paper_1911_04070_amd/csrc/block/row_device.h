@@ -63,5 +63,15 @@ bool off_boundary(P... p) {
     return (bits & 15u) != 0;
 }
 
+inline bpt_row_strides_t row_strides(const bpt_row_strides_t* given, int64_t all) {
+    return given ? *given : bpt_row_strides_t{all, all, all, all};
+}
+// rows of d elements may lie `stride` apart: they do not overlap and start on 16-byte boundaries
+inline bool stride_ok(int64_t stride, int64_t d, int64_t most) { return stride >= d && !(stride & 7) && stride <= most; }
+// a result in the place of an input has its rows in the input's places
+inline bool same_place(const void* out, const void* in, int64_t rows, int64_t out_stride, int64_t in_stride) {
+    return out != in || !out || rows <= 1 || out_stride == in_stride;
+}
+
 }  // namespace
 }  // namespace bpt

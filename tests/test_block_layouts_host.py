@@ -136,3 +136,92 @@ def test_rows_that_differ_are_refused(recorder):
                   x[:, :1].expand(1, 6, 64)):
         with pytest.raises(ValueError):
             bpt.bpt_residual_norm_fwd(x, other)
+
+
+def storage(t):
+    return t.untyped_storage().nbytes() // t.element_size()
+
+
+def slices(d=64, dtype=torch.bfloat16):
+    """[4, 1, d] tensors: dense, the last rows of longer sequences, and a part of wider rows"""
+    return [torch.zeros((4, 1, d), dtype=dtype), torch.zeros((4, 7, d), dtype=dtype)[:, -1:], torch.zeros((4, 1, 3 * d), dtype=dtype)[..., d:2 * d]]
+
+
+def test_results_take_the_memory_of_their_own_rows(recorder):
+    d, f = 64, 128
+    W = [torch.zeros((d, f), dtype=torch.bfloat16), torch.zeros((d, f), dtype=torch.bfloat16), torch.zeros((f, d), dtype=torch.bfloat16)]
+    stats = torch.zeros((4, 4))
+    for x in slices():
+        results = list(bpt.bpt_residual_norm_fwd(x, x)) + list(bpt.bpt_residual_norm_bwd(x, x, None, stats, x, x).values())
+        results += [bpt.bpt_gated_ffn_fwd(x, *W), bpt.bpt_gated_ffn_bwd(x, *W, x)[0]]
+        leaf = x.requires_grad_()
+        for out in bpt.residual_norm(leaf, leaf) + (bpt.gated_ffn(leaf, *W),):
+            results += [out, torch.autograd.grad(out, leaf, torch.zeros((4, 7, d), dtype=x.dtype)[:, 2:3], retain_graph=True)[0]]
+        assert len(results) == 12
+        for t in results:
+            assert t.shape == x.shape and t.is_contiguous() and storage(t) == x.numel()
+
+
+def test_rows_lie_where_their_tensors_say(recorder):
+    # each tensor's own distance of rows goes into the call; contiguous tensors need none
+    stats = torch.zeros((4, 4))
+    W = [torch.zeros((64, 128), dtype=torch.bfloat16), torch.zeros((64, 128), dtype=torch.bfloat16), torch.zeros((128, 64), dtype=torch.bfloat16)]
+    apart = {0: 64, 1: 448, 2: 192}
+
+    def strides():
+        name, args = [c for c in recorder.calls if c[0].endswith("_strided")][-1]
+        assert args[0].stride == 64
+        return None if args[1] is None else (args[1].x, args[1].branch, args[1].out, args[1].grad)
+
+    for i, x in enumerate(slices()):
+        for j, b in enumerate(slices()):
+            bpt.bpt_residual_norm_fwd(x, b)
+            assert strides() == (None if i == j == 0 else (apart[i], apart[j], 64, 64))
+            bpt.bpt_gated_ffn_fwd(x, *W, out=b)
+            assert strides() == (None if i == j == 0 else (apart[i], 64, apart[j], 64))
+            bpt.bpt_gated_ffn_bwd(x, *W, b)
+            assert strides() == (None if i == j == 0 else (apart[i], 64, 64, apart[j]))
+            for k, g in enumerate(slices()):
+                bpt.bpt_residual_norm_bwd(x, b, None, stats, g, g)
+                assert strides() == (None if i == j == k == 0 else (apart[i], apart[j], 64, apart[k]))
+            # dy and dh lie differently: both are made contiguous
+            bpt.bpt_residual_norm_bwd(x, x, None, stats, x, b)
+            assert strides() == (None if i == 0 else (apart[i], apart[i], 64, apart[i] if i == j else 64))
+
+
+def test_strided_calls_refuse_what_they_cannot_read():
+    L = bpt.load_library()
+    INVALID = bpt.BPT_ERR_INVALID_ARG
+    P = [4096 * (i + 1) for i in range(20)]
+    norm = bpt.BptResidualNorm(10, 64, bpt.BPT_BF16, 64, 0, 2, 0, 1.0, 0.0)
+    ffn = bpt.BptGatedFfn(10, 64, 128, bpt.BPT_BF16, 0, 64, bpt.BPT_F32)
+    grads = bpt.BptResidualNormGrads()
+
+    # (only calls that are refused are made: the pointers are made-up numbers)
+    def call(which, s, y=P[6], dx=P[9], dX=P[6]):
+        s = ctypes.byref(bpt.BptRowStrides(*s))
+        if which == "norm":
+            return L.bpt_residual_norm_fwd_strided(ctypes.byref(norm), s, P[0], P[1], None, None, None, None, None, y, P[7], None, None)
+        if which == "norm backward":
+            return L.bpt_residual_norm_bwd_strided(ctypes.byref(norm), s, P[0], P[1], None, None, None, None, None, P[6], P[7], P[8], dx, P[10],
+                                                   ctypes.byref(grads), P[15], 1 << 30, None)
+        if which == "ffn":
+            return L.bpt_gated_ffn_fwd_strided(ctypes.byref(ffn), s, *P[:4], y, P[10], 1 << 40, None)
+        return L.bpt_gated_ffn_bwd_strided(ctypes.byref(ffn), s, *P[:5], dX, *P[7:10], P[10], 1 << 40, None)
+
+    every = ("norm", "norm backward", "ffn", "ffn backward")
+    readers = (every, every[:2], every, ("norm backward", "ffn backward"))   # of x, branch, out, grad
+    for at, which in enumerate(readers):
+        for bad in (56, 68, 0, -64, 1 << 41, 1 << 20):
+            s = [64] * 4
+            s[at] = bad
+            for w in which:
+                if bad != 1 << 20 or w.startswith("ffn"):    # (the feed-forward block's offsets within a tile have 32 bits)
+                    assert call(w, s) == INVALID, (w, at, bad)
+    # a result over an input of another distance
+    for y in P[:2]:
+        assert call("norm", (64, 64, 72, 64), y=y) == INVALID
+    for dx in P[7:9]:
+        assert call("norm backward", (64, 64, 72, 64), dx=dx) == INVALID
+    for dX in (P[0], P[4]):
+        assert call("ffn backward", (64, 64, 72, 64), dX=dX) == INVALID

@@ -45,3 +45,55 @@ def test_rows_with_unit_axes():
     want = work(dense, dense)
     for place, other in ((dense, turned_round), (turned_round, dense), (turned_round, turned_round)):
         assert all(torch.equal(a, w) for a, w in zip(work(place, other), want))
+
+
+@pytest.mark.parametrize("rows,d,f", [(1, 64, 72), (5, 512, 1368), (40, 136, 264), (300, 512, 520), (4001, 264, 1032)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_each_tensor_lies_as_it_likes(rows, d, f, dtype):
+    # every tensor of a call in a layout of its own against all of them dense: the same bits; what lies around results is left alone
+    print("layouts", rows, d, f, dtype, flush=True)
+    gen = torch.Generator().manual_seed(rows + d)
+    r = lambda *s: torch.randn(s, generator=gen)
+    x, b, dy, dh = (r(rows, 1, d).to(dtype).cuda() for _ in range(4))
+    gate = r(-(-rows // 3), d).to(dtype).cuda()
+    gain, bias = (1 + 0.1 * r(d)).cuda(), (0.1 * r(d)).cuda()
+    how = dict(post="rms", pre="layer", post_gain=gain, post_bias=bias, pre_gain=gain, pre_bias=bias, gate_rows=3, residual_scale=0.75)
+    W = [(r(d, f) * d ** -0.5).bfloat16().cuda(), (r(d, f) * d ** -0.5).bfloat16().cuda(), (r(f, d) * f ** -0.5).bfloat16().cuda()]
+
+    def apart(t, before, after):      # the rows of t in the middle of longer sequences
+        frame = torch.full((rows, before + 1 + after, d), 9.0, dtype=t.dtype, device="cuda")
+        frame[:, before:before + 1] = t
+        return frame[:, before:before + 1]
+
+    def work(x, b, dy, dh):
+        y, h, stats = bpt.bpt_residual_norm_fwd(x, b, gate, want_stats=True, **how)
+        got = [y, h] + [v for _, v in sorted(bpt.bpt_residual_norm_bwd(x, b, gate, stats, dy, dh, **how).items())]
+        if dtype == torch.bfloat16:
+            got += [bpt.bpt_gated_ffn_fwd(x, *W), *bpt.bpt_gated_ffn_bwd(x, *W, dy)]
+        return got
+
+    want = work(x, b, dy, dh)
+    for place in ((6, 0, 0, 0), (0, 3, 0, 0), (0, 0, 5, 0), (0, 0, 0, 2), (2, 2, 2, 2), (1, 2, 3, 3), (3, 0, 2, 1)):
+        tensors = [apart(t, n, n // 2) if n else t for t, n in zip((x, b, dy, dh), place)]
+        got = work(*tensors)
+        assert all(torch.equal(a, w) for a, w in zip(got, want)), place
+        assert all(t.is_contiguous() for t in got)
+    if dtype == torch.bfloat16:
+        frame = torch.full((rows, 3, d), 9.0, dtype=dtype, device="cuda")
+        Y = bpt.bpt_gated_ffn_fwd(apart(x, 6, 0), *W, out=frame[:, 1:2])
+        assert torch.equal(Y, bpt.bpt_gated_ffn_fwd(x, *W))
+        assert bool((frame[:, ::2] == 9.0).all())
+
+
+def test_the_last_rows_of_long_sequences():
+    # a decoding step on what the sequences' last tokens left: 32 rows, 2^22 elements apart, beside a dense branch
+    states = torch.zeros((32, 8192, 512), dtype=torch.bfloat16, device="cuda")
+    gen = torch.Generator().manual_seed(2)
+    last = states[:, -1:]
+    last.copy_(torch.randn((32, 1, 512), generator=gen))
+    branch = torch.randn((32, 1, 512), generator=gen).bfloat16().cuda()
+    before = torch.cuda.memory_allocated()
+    y, h = bpt.bpt_residual_norm_fwd(last, branch)
+    assert torch.cuda.memory_allocated() - before <= 2 * max(32 * 512 * 2, 512) + 1024
+    want = bpt.bpt_residual_norm_fwd(last.contiguous(), branch)
+    assert torch.equal(y, want[0]) and torch.equal(h, want[1])
