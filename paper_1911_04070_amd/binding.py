@@ -927,14 +927,22 @@ def _ffn_args(X, Wg, Wu, Wd, activation, bf16_grads=False):
     return BptGatedFfn(X.numel() // d if d else 0, d, f, BPT_BF16, ACTIVATIONS[activation], d, BPT_BF16 if bf16_grads else BPT_F32)
 
 
+def _near_rows(x: torch.Tensor, what: str) -> torch.Tensor:
+    """x, copied together where its rows lie further apart than the block's products take: 2^20 elements, a slice of a long sequence."""
+    return x if x.is_contiguous() or _row_stride(x, what) < 1 << 20 else x.contiguous()
+
+
 def bpt_gated_ffn_fwd(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.Tensor, activation: str = "silu",
                       out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Y = (act(X Wg) * (X Wu)) Wd for X [..., d] bf16, rows evenly apart, Wg, Wu [d, f], Wd [f, d]; act "silu", "gelu" or "relu".  Y is
     contiguous, or `out`, whose rows lie evenly apart."""
     s = _ffn_args(X, Wg, Wu, Wd, activation)
     L = load_library()
+    X = _near_rows(X, "X")
     if out is not None:
         _like(X, out, "out")
+        if not out.is_contiguous() and _row_stride(out, "out") >= 1 << 20:
+            return out.copy_(bpt_gated_ffn_fwd(X, Wg, Wu, Wd, activation, workspace=workspace))
     strides = _row_strides(X, None, out, None, ("X", "", "out", ""))
     if out is None:
         out = _dense(X)
@@ -953,6 +961,7 @@ def bpt_gated_ffn_bwd(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: t
     in fp32 or, with bf16_grads, rounded to bf16.  dY: rows evenly apart."""
     s = _ffn_args(X, Wg, Wu, Wd, activation, bf16_grads)
     _like(X, dY, "dY")
+    X, dY = _near_rows(X, "X"), _near_rows(dY, "dY")
     strides = _row_strides(X, None, None, dY, ("X", "", "", "dY"))
     L = load_library()
     dX = _dense(X)

@@ -225,3 +225,18 @@ def test_strided_calls_refuse_what_they_cannot_read():
         assert call("norm backward", (64, 64, 72, 64), dx=dx) == INVALID
     for dX in (P[0], P[4]):
         assert call("ffn backward", (64, 64, 72, 64), dX=dX) == INVALID
+
+
+def test_rows_too_far_apart_for_the_products_are_copied_together(recorder):
+    d = 64
+    W = [torch.zeros((d, 128), dtype=torch.bfloat16), torch.zeros((d, 128), dtype=torch.bfloat16), torch.zeros((128, d), dtype=torch.bfloat16)]
+    for tokens, strides in (((1 << 20) // d - 1, (1 << 20) - d), ((1 << 20) // d, None), ((1 << 20) // d + 3, None)):
+        x = torch.zeros((3, tokens, d), dtype=torch.bfloat16)[:, -1:]
+        del recorder.calls[:]
+        assert bpt.bpt_gated_ffn_fwd(x, *W).shape == x.shape
+        assert bpt.bpt_gated_ffn_fwd(x, *W, out=x) is x
+        bpt.bpt_gated_ffn_bwd(x, *W, x)
+        for name, args in recorder.calls:
+            if name.endswith("_strided"):
+                assert (args[1] is None) == (strides is None) and (strides is None or args[1].x == strides)
+                assert (args[2] == x.data_ptr()) == (strides is not None)

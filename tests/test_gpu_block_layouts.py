@@ -97,3 +97,10 @@ def test_the_last_rows_of_long_sequences():
     assert torch.cuda.memory_allocated() - before <= 2 * max(32 * 512 * 2, 512) + 1024
     want = bpt.bpt_residual_norm_fwd(last.contiguous(), branch)
     assert torch.equal(y, want[0]) and torch.equal(h, want[1])
+    # the same rows through the feed-forward block, forward and backward
+    W = [(torch.randn(s, generator=gen) * s[0] ** -0.5).bfloat16().cuda().requires_grad_() for s in ((512, 264), (512, 264), (264, 512))]
+    leaves = [last.detach().requires_grad_(), last.contiguous().requires_grad_()]
+    got, want = ([Y] + list(torch.autograd.grad(Y, [x] + W, branch)) for x in leaves for Y in (bpt.gated_ffn(x, *W),))
+    assert all(torch.equal(a, w) for a, w in zip(got, want))
+    assert torch.equal(bpt.bpt_gated_ffn_fwd(last, *[w.detach() for w in W], out=last), want[0]) and torch.equal(last, want[0])
+    assert not bool(states[:, :-1].any())
