@@ -932,6 +932,15 @@ def _near_rows(x: torch.Tensor, what: str) -> torch.Tensor:
     return x if x.is_contiguous() or _row_stride(x, what) < 1 << 20 else x.contiguous()
 
 
+def _ffn_workspace(workspace: Optional[torch.Tensor], nbytes: int, X: torch.Tensor) -> Tuple[torch.Tensor, int]:
+    """(workspace, its bytes): the caller's, all of whose bytes have to be memory of X's device, or a new one."""
+    if workspace is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=X.device), nbytes
+    if workspace.device != X.device or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the device of X")
+    return workspace, workspace.numel() * workspace.element_size()
+
+
 def bpt_gated_ffn_fwd(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.Tensor, activation: str = "silu",
                       out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Y = (act(X Wg) * (X Wu)) Wd for X [..., d] bf16, rows evenly apart, Wg, Wu [d, f], Wd [f, d]; act "silu", "gelu" or "relu".  Y is
@@ -947,11 +956,9 @@ def bpt_gated_ffn_fwd(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: t
     if out is None:
         out = _dense(X)
     need = _need(int(L.bpt_gated_ffn_fwd_workspace(ctypes.byref(s))), "bpt_gated_ffn_fwd_workspace")
-    if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=X.device)
+    workspace, nbytes = _ffn_workspace(workspace, need, X)
     _check(L.bpt_gated_ffn_fwd_strided(ctypes.byref(s), _ref(strides), X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(), out.data_ptr(),
-                                       workspace.data_ptr(), workspace.numel() * workspace.element_size(), _raw_stream(X.device.index)),
-           "bpt_gated_ffn_fwd")
+                                       workspace.data_ptr(), nbytes, _raw_stream(X.device.index)), "bpt_gated_ffn_fwd")
     return out
 
 
@@ -967,11 +974,10 @@ def bpt_gated_ffn_bwd(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: t
     dX = _dense(X)
     dWg, dWu, dWd = (torch.empty(W.shape, dtype=torch.bfloat16 if bf16_grads else torch.float32, device=X.device) for W in (Wg, Wu, Wd))
     need = _need(int(L.bpt_gated_ffn_bwd_workspace(ctypes.byref(s))), "bpt_gated_ffn_bwd_workspace")
-    if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=X.device)
+    workspace, nbytes = _ffn_workspace(workspace, need, X)
     _check(L.bpt_gated_ffn_bwd_strided(ctypes.byref(s), _ref(strides), X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), Wd.data_ptr(), dY.data_ptr(),
-                                       dX.data_ptr(), dWg.data_ptr(), dWu.data_ptr(), dWd.data_ptr(), workspace.data_ptr(),
-                                       workspace.numel() * workspace.element_size(), _raw_stream(X.device.index)), "bpt_gated_ffn_bwd")
+                                       dX.data_ptr(), dWg.data_ptr(), dWu.data_ptr(), dWd.data_ptr(), workspace.data_ptr(), nbytes,
+                                       _raw_stream(X.device.index)), "bpt_gated_ffn_bwd")
     return dX, dWg, dWu, dWd
 
 

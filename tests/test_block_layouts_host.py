@@ -240,3 +240,21 @@ def test_rows_too_far_apart_for_the_products_are_copied_together(recorder):
             if name.endswith("_strided"):
                 assert (args[1] is None) == (strides is None) and (strides is None or args[1].x == strides)
                 assert (args[2] == x.data_ptr()) == (strides is not None)
+
+
+def test_a_workspace_of_the_callers_is_memory_of_the_device(recorder):
+    d = 64
+    W = [torch.zeros((d, 128), dtype=torch.bfloat16), torch.zeros((d, 128), dtype=torch.bfloat16), torch.zeros((128, d), dtype=torch.bfloat16)]
+    x = torch.zeros((4, d), dtype=torch.bfloat16)
+    calls = (lambda ws: bpt.bpt_gated_ffn_fwd(x, *W, workspace=ws), lambda ws: bpt.bpt_gated_ffn_bwd(x, *W, x, workspace=ws))
+    for call in calls:
+        for ws in (torch.empty(1 << 20, dtype=torch.uint8, device="meta"),        # of another device
+                   torch.zeros(1, dtype=torch.uint8).expand(1 << 20),             # one byte, counted a million times
+                   torch.zeros(1 << 21, dtype=torch.uint8)[::2]):                 # bytes in between that are not the workspace's
+            del recorder.calls[:]
+            with pytest.raises(ValueError, match="workspace"):
+                call(ws)
+            assert not any(name.endswith("_strided") for name, _ in recorder.calls)
+        ws = torch.empty((16, 100), dtype=torch.float32)
+        call(ws)
+        assert recorder.calls[-1][1][-3:-1] == [ws.data_ptr(), 6400]
