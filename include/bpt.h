@@ -432,7 +432,7 @@ int bpt_rotary(const bpt_rotary_t* s, const float* pos, int64_t pos_stride_b, co
 /* pos[row] of every row of the graph, for bpt_rotary: the centre of the tokens that a node stands for, m 2^l + (2^l - 1) / 2
  * for node (l, m) -- a token's own index, halves for spans -- counted from the start of its own sequence on the
  * graph of a packed batch (nodes cut short by their sequence's end keep the centre of the whole node, as they have on the
- * padded tree).  pos: device, num_nodes fp32. */
+ * padded tree).  pos: num_nodes fp32 on the graph's device, which has to be the current one. */
 int bpt_node_positions(const bpt_graph_t* g, float* pos, void* stream);
 
 /* Elements between the rows of a call's tensors where these do not all lie alike (a slice of a larger tensor beside a dense one):

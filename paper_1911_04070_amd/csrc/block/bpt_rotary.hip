@@ -253,6 +253,9 @@ int bpt_rotary(const bpt_rotary_t* s, const float* pos, int64_t pos_stride_b, co
 
 int bpt_node_positions(const bpt_graph_t* g, float* pos, void* stream) {
     if (!g || !pos || off_boundary(pos)) return BPT_ERR_INVALID_ARG;
+    int device = 0;
+    BPT_HIP(hipGetDevice(&device));
+    if (device != g->device) return BPT_ERR_INVALID_ARG;   // (a batch graph's tables are the memory of its own)
     hipStream_t st = static_cast<hipStream_t>(stream);
     const UseOnReturn use = {g, st};
     PositionArgs a = {};

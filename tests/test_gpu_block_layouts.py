@@ -104,3 +104,12 @@ def test_the_last_rows_of_long_sequences():
     assert all(torch.equal(a, w) for a, w in zip(got, want))
     assert torch.equal(bpt.bpt_gated_ffn_fwd(last, *[w.detach() for w in W], out=last), want[0]) and torch.equal(last, want[0])
     assert not bool(states[:, :-1].any())
+
+
+@pytest.mark.skipif(torch.cuda.device_count() < 2, reason="needs two devices")
+def test_positions_of_a_graph_on_another_device_are_refused():
+    g = bpt.bpt_build_batch_graph(64, 2, True, [5, 64])
+    with torch.cuda.device(1), pytest.raises(bpt.BptError):
+        bpt.bpt_node_positions(g)
+    assert bpt.bpt_node_positions(g).shape == (g.num_nodes,)
+    g.destroy()
