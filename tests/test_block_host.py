@@ -177,3 +177,19 @@ def test_rows_that_lie_evenly_apart():
               base[:, :1].expand(4, 6, 24), base[0, :1].expand(6, 24)):
         with pytest.raises(ValueError):
             bpt._row_stride(x, "x")
+
+
+def test_gated_ffn_workspaces_of_every_shape_the_calls_take():
+    # refused exactly where a launch would have too many tiles; else room for the hidden activations (three of them backward) and sums
+    L = bpt.load_library()
+    refused = 0
+    for rows in (0, 1, 7, 1000, 8191, 1 << 20, (1 << 23) - 64, 1 << 23):
+        for d, f in ((8, 8), (64, 128), (2048, 8), (8, 65536), (4096, 16384), (65536, 65536)):
+            tiles = max(-(-rows // 64) * -(-d // 64), -(-rows // 128) * -(-f // 128))
+            refused += tiles >= 1 << 23
+            for query, hidden in ((L.bpt_gated_ffn_fwd_workspace, 1), (L.bpt_gated_ffn_bwd_workspace, 3)):
+                need = query(ctypes.byref(struct(bpt.BptGatedFfn, FFN, rows=rows, d=d, f=f, stride=d)))
+                assert (need == SIZE_MAX) == (tiles >= 1 << 23), (rows, d, f)
+                # (hidden activations in two parts at most; sums of parts: as many tiles as the device holds at once, 64 MB)
+                assert need == SIZE_MAX or hidden * 2 * rows * f <= need <= hidden * 4 * rows * f + (1 << 27)
+    assert refused > 0

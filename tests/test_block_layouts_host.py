@@ -57,7 +57,8 @@ def test_rotary_takes_unit_axes_of_any_stride(recorder, shape):
             if bpt._head_strides(Q) != bpt._head_strides(K):
                 continue
             Qr, Kr = bpt.bpt_rotary(Q, K, pos)
-            bpt.bpt_rotary(Q, K, pos, out=(K, Q))
+            bpt.bpt_rotary(Q, K, pos, out=(Qr, Kr))
+            bpt.bpt_rotary(Q, K, pos, out=(Q, K))
             assert Qr.shape == Kr.shape == Q.shape
             assert bpt._head_strides(Qr) == bpt._head_strides(Kr)
 

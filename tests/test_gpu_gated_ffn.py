@@ -224,3 +224,19 @@ def test_rows_far_into_memory():
         for k in ("dWg", "dWu", "dWd"):
             want[k] = part[k] if k not in want else tuple(a + b for a, b in zip(want[k], part[k]))
     check({k: got[k] for k in want}, want)
+
+
+def test_rows_beside_one_that_is_not_finite_keep_their_bits():
+    # forward and backward, against the calls before anything was poisoned (the weights' gradients take all rows in)
+    for rows in (3, 40, 300, 9000):
+        X, dY, W = make(rows, 192, 520, rows)
+        want = both(X, dY, W, "gelu", False)
+        for which, value in ((X, float("nan")), (dY, float("inf"))):
+            kept = which[1].clone()
+            which[1, 5] = value
+            got = both(X, dY, W, "gelu", False)
+            which[1] = kept
+            rest = torch.arange(rows, device="cuda") != 1
+            for k in ("Y", "dX"):
+                assert torch.equal(got[k][rest], want[k][rest]), (rows, k)
+            assert not bool(torch.isfinite(got["dX"][1]).any())

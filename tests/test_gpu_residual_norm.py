@@ -280,3 +280,22 @@ def test_second_derivatives_are_refused():
     g, = torch.autograd.grad(h.square().sum(), x, create_graph=True)
     with pytest.raises(RuntimeError):
         torch.autograd.grad(g.sum(), x)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,d", [(40, 64), (40, 512), (37, 1032), (300, 24)])
+def test_rows_beside_one_that_is_not_finite_keep_their_bits(rows, d, dtype):
+    # what the other rows have is compared with the call before anything was poisoned
+    for post, pre in (("rms", "rms"), ("layer", "layer"), ("none", "rms")):
+        c, t = make(rows, d, dtype, post, pre, 1, rows + d)
+        want = call(c, t)
+        for i, (name, value) in enumerate((("branch", float("nan")), ("x", float("inf")), ("dy", float("nan")), ("dh", float("-inf")),
+                                           ("gate", float("inf")))):
+            row = (7 * i + 3) % rows
+            poisoned = dict(t, **{name: t[name].clone()})
+            poisoned[name][row, d // 2 + 1] = value
+            got = call(c, poisoned)
+            rest = torch.arange(rows, device="cuda") != row
+            for k in ("y", "h", "dx", "d_branch", "d_gate"):
+                assert torch.equal(got[k][rest], want[k][rest]), (post, pre, name, k)
+            assert not bool(torch.isfinite(got["dx"][row]).all()), (post, pre, name)
