@@ -759,7 +759,7 @@ def bpt_rotary(Q: torch.Tensor, K: Optional[torch.Tensor], pos: torch.Tensor, ro
                inverse: bool = False, out=None):
     """Qr, Kr = rotary positions on Q and K [B,H,N,64] (K may be None; any strides with the features contiguous): the first
     `rot` features of every head (all by default) are turned by pos * base^(-2 i / rot), with `factor`, `context`, `low` and
-    `high` for contexts longer than those a model was made for (see include/bpt.h).  pos: fp32 [N] or [B, N].  inverse: the other
+    `high` for contexts longer than those a model was made for (see include/bpt.h; base <= 0 selects 10000, factor <= 0 selects 1).  pos: fp32 [N] or [B, N].  inverse: the other
     way, which is the gradient.  out: a pair of tensors to write, which may be (Q, K) themselves."""
     dev = _on_device(Q, "Q")
     if Q.dim() != 4 or Q.stride(3) != 1:
@@ -864,7 +864,7 @@ def bpt_residual_norm_fwd(x: torch.Tensor, branch: Optional[torch.Tensor], gate:
                           residual_scale: float = 1.0, eps: float = 1e-5, want_stats: bool = False):
     """y = residual_scale * x + gate * post(branch) and h = pre(y), post and pre "layer", "rms" or "none" (then h is None).
     x, branch: [..., d] in fp32 or bf16, rows evenly apart; gate: [ceil(rows / gate_rows), d] in their type, each row for gate_rows
-    consecutive rows; gains and biases fp32 [d] or None.  Results are contiguous.
+    consecutive rows; gains and biases fp32 [d] or None.  Results are contiguous.  eps <= 0 selects 1e-5.
     Returns (y, h), with want_stats (y, h, stats) for the backward."""
     s = _norm_args(x, branch, gate, post, pre, post_gain, post_bias, pre_gain, pre_bias, gate_rows, residual_scale, eps)
     strides = _row_strides(x, branch, None, None, ("x", "branch", "y", "dy"))
@@ -944,7 +944,8 @@ def _ffn_workspace(workspace: Optional[torch.Tensor], nbytes: int, X: torch.Tens
 def bpt_gated_ffn_fwd(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.Tensor, activation: str = "silu",
                       out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Y = (act(X Wg) * (X Wu)) Wd for X [..., d] bf16, rows evenly apart, Wg, Wu [d, f], Wd [f, d]; act "silu", "gelu" or "relu".  Y is
-    contiguous, or `out`, whose rows lie evenly apart."""
+    contiguous, or `out`, whose rows lie evenly apart.  The hidden activations are rounded to bf16 before the last product (few rows keep
+    16 bits of them)."""
     s = _ffn_args(X, Wg, Wu, Wd, activation)
     L = load_library()
     X = _near_rows(X, "X")

@@ -21,7 +21,7 @@ __device__ __forceinline__ void activation(float g, float& value, float& slope) 
     } else if constexpr (ACT == BPT_ACT_GELU) {
         // Phi(-|g|) = exp(-g^2 / 2) t q(t), t = 1 / (1 + 0.3 |g|): q is a polynomial of degree 7 fitted (least squares, weights
         // moved to level the error) to the scaled complementary error function over |g| <= 14, 1.5e-7 relative; with fp32
-        // arithmetic 2e-6 relative for |g| <= 6, where erff and the exponential of the slope would cost twice the instructions
+        // arithmetic below 3e-6 relative for |g| <= 6, where erff and the exponential of the slope would cost twice the instructions
         const float e = __builtin_amdgcn_exp2f(g * g * -0.72134752044448170f);
         const float t = __builtin_amdgcn_rcpf(fmaf(0.3f, fabsf(g), 1.f));
         float q = 0.035674779f;
@@ -61,9 +61,12 @@ __device__ __forceinline__ void store4(float* p, float a, float b, float c, floa
 
 // ---- F = act(X Wg) * (X Wu) ---------------------------------------------------------------------------------
 // One product whose tiles hold the same columns of both projections, so that activation and product are formed from the fp32
-// sums where they lie.  65 532 rows, d = 512, f = 2048: 300 us, 0.92 PFLOP/s (250 us without what follows the sums: an
-// exponential and a reciprocal at a quarter of the rate for each value, and 268 MB written); 9001 rows, d = 2048,
-// f = 5464: 379 us, 1.06 PFLOP/s.
+// sums where they lie.  65 532 rows, d = 512, f = 2048: 300 to 314 us over devices, 0.92 to 0.88 PFLOP/s (250 us without what follows
+// the sums: an exponential and a reciprocal at a quarter of the rate for each value, and 268 MB written); 9001 rows, d = 2048,
+// f = 5464: 384 us, 1.05 PFLOP/s.
+// F is rounded to bf16, the type of the next product's operand.  That rounding and Y's own are alike in size and independent: Y is off
+// by sqrt(2) times its own rounding in the 2-norm (2.3e-3 instead of 1.7e-3 measured, whatever the size).  A second bf16 part, as the
+// strips for few rows write it, would take this away and cost the next product twice its operations and F twice its bytes.
 struct UpArgs {
     const bf16_t *X, *Wg, *Wu;
     bf16_t *F, *F_low;    // (F_low: strips only)
@@ -191,8 +194,8 @@ __global__ void __launch_bounds__(256) down_sum_kernel(const DownArgs g) {
 
 // ---- C = A0 B0 (+ A1 B1), or several products side by side ------------------------------------------------------
 // The first `full` tiles are computed whole; what is left over is less than the device holds at once and is cut into
-// `slices` of k, whose sums go to `part` and are added by product_sum_kernel, in order.  65 532 rows, d = 512, f = 2048: Y 135 us
-// (1.0 PFLOP/s), dX 255 us, dWg and dWu 266 + 13 us; 9001 rows, d = 2048, f = 5464: dX 410 us in 256 whole tiles and 32 in
+// `slices` of k, whose sums go to `part` and are added by product_sum_kernel, in order.  65 532 rows, d = 512, f = 2048: Y 139 us
+// (1.0 PFLOP/s), dX 264 us, dWg and dWu 269 + 13 us; 9001 rows, d = 2048, f = 5464: dX 429 us in 256 whole tiles and 32 in
 // eight slices each (608 us in two rounds of whole tiles).
 struct ProductArgs {
     const bf16_t *A[2], *B[2];
@@ -346,8 +349,10 @@ struct HiddenArgs {
 // G = X Wg and U = X Wu are formed again, then dF = dY Wd^T on the same tile: F, dG and dU are written, rounded once.  G and U could
 // be kept by the forward instead, but not rounded to bf16 (with both rounded dX is off by 1.9 times the rounding of dX itself;
 // now 1.4 times), and in fp32 they cost 16 bytes of traffic per value against 4 d operations: even at d = 800 or so, below which
-// most widths here lie, and no gigabyte of activations is held per layer.  65 532 rows, d = 512, f = 2048: 555 us, 0.74
-// PFLOP/s (805 MB written); 9001 rows, d = 2048, f = 5464: 650 us, 0.93 PFLOP/s.
+// most widths here lie, and no gigabyte of activations is held per layer.  F, dG and dU are rounded to bf16 as the forward's F is.
+// 65 532 rows, d = 512, f = 2048: 567 to 589 us over devices, 0.73 to 0.70 PFLOP/s (805 MB written); 9001 rows, d = 2048, f = 5464:
+// 664 to 688 us, 0.91 to 0.88 PFLOP/s.  The matrix cores are busy 34 % of the cycles, the least of the block's large products at no lower
+// a clock: one workgroup per compute unit lets its loads run dry between the two sums and writes with nothing else running.
 template <typename C, typename C2, int ACT>
 __global__ void __launch_bounds__(C::kThreads, C::kWavesPerSimd) gated_hidden_bwd_kernel(const HiddenArgs g) {
     __shared__ __attribute__((aligned(1024))) unsigned char shared[C::kLds > C2::kLds ? C::kLds : C2::kLds];
@@ -516,7 +521,8 @@ dim3 strip_grid(int64_t rows, int cols) { return dim3((unsigned)((cols + 31) / 3
 // Tiles of the hidden activations: 128 rows by 128 columns of both halves, or by 64 where these leave compute units idle, or
 // 64 rows by 64 columns where those have a compute unit each (d = 512, f = 1368, 300 rows: 7.2 -> 6.0 us forward, 11.8 -> 9.5 us
 // backward; 1023 rows 7.6 -> 10.9 us, 13.6 -> 18.1 us); backward 256 rows by 128 columns for two rounds and more (65 532 rows,
-// d = 512, f = 2048: 573 -> 560 us; forward 309 -> 319 us, 9001 rows, d = 2048, f = 5464: 383 -> 392 us)
+// d = 512, f = 2048: 573 -> 560 us; forward 309 -> 319 us, 9001 rows, d = 2048, f = 5464: 383 -> 392 us).  How full the last
+// round is does not enter, here or in the forward: 65 532 rows are 16.0 rounds of the backward's tiles; the 9001 are 6.05, which cost seven.
 enum HiddenSize { kHiddenBig, kHiddenWide, kHiddenMid, kHiddenSmall };
 HiddenSize hidden_tiles(int64_t M, int f, bool backward, int32_t& tiles_m, int32_t& tiles_n) {
     auto count = [&](int m, int n) {

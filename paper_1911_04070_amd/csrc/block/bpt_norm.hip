@@ -15,7 +15,8 @@ namespace {
 // 64, 128, 256, 512 (1 to 8 wavefronts) that covers d, so that the row stays in registers between its passes whatever d is; a
 // workgroup of 256 threads (or THREADS) works on several rows side by side.  (Other multiples of 64 leave fewer threads idle and
 // compute units worse filled: 30 000 rows of 1032 in bf16, backward with 192 threads 183 us, with 256 131 us.  500 000 rows of 64 in
-// bf16 with 16 threads a row: forward 70 us, with its backward 199 us; with 8: 44 and 143 us.)
+// bf16 with 16 threads a row: forward 70 us, with its backward 199 us; with 8: 44 and 143 us.)  Just above a power of two nearly half
+// the threads have no columns and as many bytes less are on their way: those 30 000 rows' bytes alone would take the backward 76 us.
 struct NormArgs {
     const void *x, *branch, *gate, *dy, *dh;
     const float *post_gain, *post_bias, *pre_gain, *pre_bias;
@@ -102,7 +103,7 @@ __device__ __forceinline__ void params8(const float* p, int col, bool has, float
 // Bound by HBM: x and branch in, y and h out, the row in registers in between; parameters of a thread's columns stay in
 // registers, the next row is loaded before the current one's sums are exchanged.  65 532 rows of 512 in bf16, a gate row for every
 // 16 383: 49 us, 5.5 TB/s (a large copy reaches 4.9 on the same device; part of what it moves is still in the memory-side
-// cache); 4095 rows of 2048 in fp32: 33 us, 4.1 TB/s.
+// cache); 4095 rows of 2048 in fp32: 28 us, 4.9 TB/s.  92 to 114 registers, none spilled.
 template <typename T, int THREADS>
 __global__ void __launch_bounds__(RowTeam<THREADS>::kBlock, sizeof(T) == 2 ? 5 : 4) residual_norm_kernel(const NormArgs a) {
     using Team = RowTeam<THREADS>;
@@ -163,7 +164,10 @@ __global__ void __launch_bounds__(RowTeam<THREADS>::kBlock, sizeof(T) == 2 ? 5 :
 // and column sums dN bhat, dN, dh yhat, dh for gains and biases.  x and branch are read again (y is formed from them in
 // fp32 as the forward did, not from its rounded copy), six values of memory traffic per element; the sums stay in the
 // thread's registers over all rows of its workgroup, which leaves two wavefronts per SIMD: rows have to be requested early.
-// 65 532 rows of 512 in bf16: 93 us, 4.3 TB/s (one row ahead instead of two: 100 us); 4095 rows of 2048 in fp32: 40 us, 5.0 TB/s.
+// 65 532 rows of 512 in bf16: 89 us, 4.5 TB/s (one row ahead instead of two: 100 us); 4095 rows of 2048 in fp32: 42 us, 4.7 TB/s.
+// A unit's rows are requested when it begins, and its gate row's sum is taken over all teams, so that gates of very few rows leave
+// teams idle and wait for memory once per gate row: 65 532 rows of 64, bf16, 27 us with a gate for every row, 263 us with one for
+// every two; of 512, 149 us with one for every three.
 // A row's number as a new value to the compiler, which else keeps a running offset in registers for every tensor and row on its way
 // (with strides of their own for the tensors 256 registers and up to 9 spilled; so 218 to 240 and none)
 __device__ __forceinline__ uint32_t hidden(uint32_t v) {
@@ -331,7 +335,7 @@ __global__ void __launch_bounds__(RowTeam<THREADS>::kBlock, 2) residual_norm_bwd
 
 // Column sums of up to 4 + gate rows of tables: job j < num_sums adds `parts` rows of part, `num_sums` rows apart; job
 // num_sums + g adds the `slices` rows of gate row g.  A workgroup takes 32 columns, 8 lanes of 16 bytes per row, 32 rows
-// in flight; sums are added across lanes and wavefronts in a fixed tree.  512 rows of 2 x 512 and 4 x 128 of 512: 5 us.
+// in flight; sums are added across lanes and wavefronts in a fixed tree.  512 rows of 2 x 512 and 4 x 128 of 512: 4 us.
 struct SumJobs {
     const float *part, *gate_part;
     float* out[4];

@@ -50,8 +50,8 @@ enum PairLayout { kNeighbours, kHalves, kHalvesApart };   // kHalvesApart: a hal
 // head's row, the next lanes the next head or the next row, whichever lies behind it, so that loads and stores are whole cache
 // lines.  With halves a thread also loads the 16 bytes its features are paired with, which its neighbours have just asked
 // for, and computes its own side of the pairs only.  Bound by HBM: 4 x 16 383 rows of 8 heads of Q and K in bf16, out of the rows a
-// projection writes: 62 us, 4.3 TB/s (lanes that hold both halves of a pair, in 64 bytes of two cache lines, and form the
-// angles of their own pairs: 80 us); 2 x 4095 rows of 8 heads in fp32: 12 us, out of the memory-side cache.
+// projection writes: 64 us, 4.2 TB/s (lanes that hold both halves of a pair, in 64 bytes of two cache lines, and form the
+// angles of their own pairs: 80 us); 2 x 4095 rows of 8 heads in fp32: 13 us, out of the memory-side cache.
 // A result may overwrite its input: a pair's threads are lanes of one wavefront, which loads before it stores.
 constexpr int kRotaryRows = 16;
 template <typename T, PairLayout LAYOUT, int NT>
